@@ -75,7 +75,11 @@ typedef enum {
     MKV_ERR_DEVICE_CHECK = 8  /* device: an internal consistency check failed         */
 } mkv_status;
 
-typedef enum { MKV_BF16 = 0, MKV_F32 = 1 } mkv_dtype;
+typedef enum {
+    MKV_BF16 = 0,
+    MKV_F32 = 1,
+    MKV_INT4 = 2 /* paged caches only */
+} mkv_dtype;
 
 /* Which heads Eq. 4 (Sec. 4.2, "Momentum-Based Attention Aggregation") averages. */
 typedef enum {
@@ -399,6 +403,124 @@ mkv_status mkv_debug_inject(mkv_ctx* ctx, int layer, int what, int b, int kv_hea
  */
 mkv_status mkv_recency_diagnostics(mkv_ctx* ctx, int layer, int window, float* mass, int32_t* count,
                                    float* curve, void* stream);
+
+/* ---- paged cache -----------------------------------------------------------------------
+ *
+ * A cache of fixed-size pages next to the contexts' pools, for the tokens of requests that are
+ * not (or not yet) in a Moment-KV context: prompts that are being worked through, sequences that
+ * are decoded without a budget.  Tokens are appended with the position rotation applied on the
+ * way, attended over, and read back as rows in the layout mkv_prefill() takes.
+ *
+ * Cache types: MKV_BF16, MKV_F32 (plain rows), MKV_INT4 (4-bit codes, 32 channels of a token
+ * sharing a bf16 scale and a bf16 lowest value: value = lowest + scale * code, with
+ * lowest = bf16(min), scale = bf16((max - min) / 15), code = rint((x - lowest) / scale) within
+ * 0..15 and 0 where scale is 0; computed in 64 bits up to the code.  A group of 32 channels that
+ * holds a NaN or an infinity becomes NaN as a whole.)
+ *
+ * pages: device memory [layers][n_pages][page], owned by the caller, 16-byte aligned, it has to
+ * outlive the handle.  A page is mkv_paged_page_bytes() long:
+ *   MKV_BF16, MKV_F32   [2 (K, V)][kv_heads][page_size][head_dim]
+ *   MKV_INT4            [kv_heads][page_size / 16 blocks], a block of 16 tokens being
+ *       K codes   32-bit words [token][t 0..3][group j]: channels 32 j + 8 t + 0..7, low nibble first
+ *       V codes   32-bit words [token pair][g 0..7][group j]: low half = channels 32 j + 4 g + 0..3 of
+ *                 the even token, high half = the same channels of the odd token
+ *       K scale   bf16 [token pair][group][token of the pair]
+ *       K lowest  bf16 [token][group]
+ *       V scale   as K scale
+ *       V lowest  as K scale
+ * Never-written rows may hold anything.
+ *
+ * A call's batch.  Every call takes the same description of its sequences:
+ *   lens    device int32 [batch]: tokens in the cache, the call's new ones included
+ *   table   device int32 [batch][table_stride]: page of position p of sequence b is
+ *           table[b][p / page_size]; entries behind lens are not read.  Sequences may share pages
+ *           they only read.  Two new tokens of one call must not have the same place.
+ *   starts  device int32 [batch + 1]: sequence b's new tokens are rows [starts[b], starts[b + 1])
+ *           of the token buffers (q, k, v, q_out, out, lse); their positions end at lens[b] - 1.
+ *           NULL: one new token per sequence (n_tokens == batch).  Rows outside
+ *           [starts[0], starts[batch]) belong to no sequence and are left as they were, so a
+ *           padded batch (recorded into a CUDA graph, say) gives spare rows no sequence, or spare
+ *           sequences lens 0.
+ * The arrays are read by the kernels.  What they find wrong sets the sticky status word of
+ * mkv_paged_status_sync(), never faults: a sequence longer than its table row (MKV_ERR_CAPACITY:
+ * the tokens beyond it are neither stored nor attended), a page number outside the pool
+ * (MKV_ERR_INVALID_ARG: the token is not stored; attention over it is undefined), starts that
+ * decrease or leave the token buffers (MKV_ERR_INVALID_ARG).
+ *
+ * Calls only enqueue kernels and can be recorded into CUDA graphs.  Calls of one handle share its
+ * workspace: they have to be on one stream or ordered by the caller, replays of recordings too
+ * (concurrent callers use a handle each; handles may share pages).
+ */
+typedef struct mkv_paged mkv_paged; /* opaque, host-owned */
+
+#define MKV_ROTATE_HALVES 0     /* channel i turns with channel i + rot_dim / 2 */
+#define MKV_ROTATE_NEIGHBOURS 1 /* channel 2 i turns with channel 2 i + 1       */
+
+/* Bytes of one page of one layer; 0 for a shape without a kernel.  head_dim 64 or 128,
+ * page_size 16, 32, 64, 128 or 256. */
+size_t mkv_paged_page_bytes(int kv_heads, int head_dim, int page_size, int kv_dtype);
+/* Bytes of the handle's workspace; 0 for a shape without a kernel.  q_heads / kv_heads <= 32. */
+size_t mkv_paged_workspace_bytes(int q_heads, int kv_heads, int head_dim, int max_batch);
+
+/* kv_dtype: the cache; io_dtype: q, k, v, q_out and the rows of mkv_paged_read (that of the cache,
+ * or either with MKV_INT4); out_dtype: attention's out (MKV_F32 where io_dtype is).  workspace:
+ * device memory, 256-byte aligned, it has to outlive the handle.  Synchronises the device.
+ * Errors: INVALID_ARG (pages_bytes too small among them), UNSUPPORTED, WORKSPACE, CUDA. */
+mkv_status mkv_paged_create(int layers, int q_heads, int kv_heads, int head_dim, int page_size, int n_pages,
+                            int max_batch, int kv_dtype, int io_dtype, int out_dtype, void* pages, size_t pages_bytes,
+                            void* workspace, size_t workspace_bytes, int device, mkv_paged** out);
+void mkv_paged_destroy(mkv_paged* ctx);
+
+/* The rotation mkv_paged_append() applies: at position t, pair i of the first rot_dim channels
+ * turns by the angle t * inv_freq[i] (formed in 64 bits).  inv_freq: host float [rot_dim / 2].
+ * rot_dim a multiple of 16, 0 (the state after create) = none.  Synchronises the device. */
+mkv_status mkv_paged_set_rotation(mkv_paged* ctx, const float* inv_freq, int rot_dim, int style);
+
+/* Stores the new tokens' keys (rotated) and values in the cache, and writes the rotated queries.
+ *   q     [n_tokens] rows of [q_heads][head_dim] io_dtype, q_stride elements apart; NULL: none
+ *   k, v  [n_tokens] rows of [kv_heads][head_dim], likewise (the three may be slices of one buffer)
+ *   q_out [n_tokens][q_heads][head_dim], may be q itself where q_stride is q_heads * head_dim;
+ *         NULL exactly when q is
+ *   positions  device int32 [n_tokens], what the rotation takes for the tokens' positions; NULL:
+ *         their positions in the cache
+ * Pointers 16-byte aligned, strides multiples of 16 bytes.  Tokens of a sequence that has fewer
+ * tokens in the cache than new ones (lens < starts[b + 1] - starts[b]) have no place for the first
+ * of them; those are passed over, their q_out rows too.
+ * Errors: INVALID_ARG, CAPACITY (batch > max_batch), CUDA. */
+mkv_status mkv_paged_append(mkv_paged* ctx, int layer, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                            const void* v, int64_t v_stride, void* q_out, int n_tokens, int batch,
+                            const int32_t* starts, const int32_t* lens, const int32_t* table, int table_stride,
+                            const int32_t* positions, void* stream);
+
+/* Attention of the new tokens' queries over the cache (which holds the new tokens already): the
+ * token at position t sees the positions j <= t, with window > 0 those with j > t - window.
+ *   q    rows as in mkv_paged_append, rotated already
+ *   out  [n_tokens][q_heads][head_dim], out_dtype
+ *   lse  float [n_tokens][q_heads] or NULL: log of the sum of exp(scale * q . k) over the seen tokens
+ *   max_new  the most new tokens any sequence has (a promise: a sequence with more sets
+ *        MKV_ERR_CAPACITY and its results are undefined); ignored where starts is NULL
+ *   scale    0: 1 / sqrt(head_dim)
+ * A token that sees nothing gets out = 0, lse = -inf.  What it does not see has no influence on a
+ * token's result, NaN and infinities included.
+ * Errors: INVALID_ARG, CAPACITY (batch > max_batch), CUDA. */
+mkv_status mkv_paged_attend(mkv_paged* ctx, int layer, const void* q, int64_t q_stride, void* out, float* lse,
+                            int n_tokens, int batch, const int32_t* starts, int max_new, const int32_t* lens,
+                            const int32_t* table, int table_stride, float scale, int window, void* stream);
+
+/* The rows of positions [first[b], lens[b]) of every sequence, as values:
+ *   K, V   [batch][kv_heads][rows][head_dim] io_dtype, row i = position first[b] + i; rows behind
+ *          are left as they were (with first = NULL, i.e. 0, this is the source mkv_prefill takes)
+ *   first  device int32 [batch] or NULL
+ * More than `rows` of them in a sequence: the first `rows` are written and MKV_ERR_CAPACITY set. */
+mkv_status mkv_paged_read(mkv_paged* ctx, int layer, int batch, const int32_t* first, const int32_t* lens,
+                          const int32_t* table, int table_stride, void* K, void* V, int rows, void* stream);
+
+/* Waits for `stream` and returns the status word. */
+mkv_status mkv_paged_status_sync(mkv_paged* ctx, void* stream);
+/* Clears the status word; the cache stays.  Synchronises the device. */
+mkv_status mkv_paged_reset(mkv_paged* ctx);
+/* Number of kernels this handle has launched so far (host counter). */
+int64_t mkv_paged_launch_count(const mkv_paged* ctx);
 
 /* ---- inspection: synchronous (device-wide sync + D2H), for tests and debugging ---- */
 

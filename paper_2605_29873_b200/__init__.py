@@ -5,4 +5,5 @@ from .mkv import (  # noqa: F401
     MKV_OPT_OVERLAP, MKV_OPT_GRID_SHARE, MKV_INJECT_LOST_TILE, grid_limit, plan_ranges,
     MKV_SCORE_GROUP_MEAN, MKV_SCORE_LAYER_MEAN, MkvError, MomentKV, load_library, workspace_bytes,
     kv_bytes_per_token, status_string, EXPORTED_SYMBOLS, attend_noalloc, plan_starts,
+    MKV_INT4, MKV_ROTATE_HALVES, MKV_ROTATE_NEIGHBOURS, PagedKV, paged_page_bytes, paged_workspace_bytes,
 )

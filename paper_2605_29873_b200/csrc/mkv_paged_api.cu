@@ -1,0 +1,236 @@
+// C ABI of the paged cache: argument checks, workspace, launches.
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+#include "mkv_paged.cuh"
+
+using namespace mkv;
+
+struct mkv_paged {
+    int layers, q_heads, kv_heads, head_dim, page_size, n_pages, max_batch;
+    int kv_dtype, io_dtype, out_dtype, device;
+    uint8_t *pages, *ws;
+    int rot_dim, interleaved;
+    int64_t launches;
+};
+
+namespace {
+
+struct PagedWs { size_t status, inv_freq, scratch, total; };
+PagedWs paged_ws() {
+    PagedWs w;
+    w.status = 0;
+    w.inv_freq = 256;
+    w.scratch = 512;
+    w.total = w.scratch;
+    return w;
+}
+
+int elem(int dt) { return dt == MKV_F32 ? 4 : 2; }
+
+bool shape_ok(int kv_heads, int head_dim, int page_size, int kv_dtype) {
+    return kv_heads >= 1 && kv_heads <= 65535 && (head_dim == 64 || head_dim == 128) && page_size >= 16 &&
+           page_size <= 256 && (page_size & (page_size - 1)) == 0 &&
+           (kv_dtype == MKV_BF16 || kv_dtype == MKV_F32 || kv_dtype == MKV_INT4);
+}
+
+struct DeviceGuard {
+    int prev = -1; bool ok;
+    explicit DeviceGuard(int dev) {
+        ok = cudaGetDevice(&prev) == cudaSuccess;
+        if (ok && prev != dev) ok = cudaSetDevice(dev) == cudaSuccess;
+    }
+    ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
+};
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+// a token's row of `heads` heads, reached every `stride` elements, as 16-byte pieces
+bool strided_ok(const mkv_paged* c, const void* p, int64_t stride, int heads) {
+    return p && aligned16(p) && stride >= (int64_t)heads * c->head_dim && (stride * elem(c->io_dtype)) % 16 == 0;
+}
+
+PagedDev dev_of(const mkv_paged* c, int layer) {
+    PagedDev d;
+    d.page_bytes = mkv_paged_page_bytes(c->kv_heads, c->head_dim, c->page_size, c->kv_dtype);
+    d.pages = c->pages + (size_t)layer * c->n_pages * d.page_bytes;
+    if (c->kv_dtype == MKV_INT4) {
+        d.head_bytes = d.page_bytes / c->kv_heads;
+        d.kv_bytes = 0;
+    } else {
+        d.head_bytes = (size_t)c->page_size * c->head_dim * elem(c->kv_dtype);
+        d.kv_bytes = d.head_bytes * c->kv_heads;
+    }
+    d.status = (int32_t*)(c->ws + paged_ws().status);
+    d.n_pages = c->n_pages;
+    d.page_shift = 0;
+    while ((1 << d.page_shift) < c->page_size) ++d.page_shift;
+    d.q_heads = c->q_heads; d.kv_heads = c->kv_heads; d.group = c->q_heads / c->kv_heads;
+    d.kv_dtype = c->kv_dtype; d.io_f32 = c->io_dtype == MKV_F32; d.out_f32 = c->out_dtype == MKV_F32;
+    return d;
+}
+
+mkv_status batch_args(const mkv_paged* c, int layer, int n_tokens, int batch, const int32_t* starts,
+                      const int32_t* lens, const int32_t* table, int table_stride) {
+    if (!c || layer < 0 || layer >= c->layers || n_tokens < 0 || batch < 0) return MKV_ERR_INVALID_ARG;
+    if (batch > c->max_batch) return MKV_ERR_CAPACITY;
+    if (!starts && n_tokens != batch) return MKV_ERR_INVALID_ARG;
+    if (n_tokens > 0 && batch == 0) return MKV_ERR_INVALID_ARG;
+    if (batch > 0 && (!lens || !table || table_stride < 1)) return MKV_ERR_INVALID_ARG;
+    if ((int64_t)table_stride * c->page_size > (1 << 30)) return MKV_ERR_UNSUPPORTED;
+    return MKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t mkv_paged_page_bytes(int kv_heads, int head_dim, int page_size, int kv_dtype) {
+    if (!shape_ok(kv_heads, head_dim, page_size, kv_dtype)) return 0;
+    if (kv_dtype == MKV_INT4) return (size_t)kv_heads * (page_size / kPagedBlock) * paged_block_bytes(head_dim);
+    return (size_t)2 * kv_heads * page_size * head_dim * elem(kv_dtype);
+}
+
+size_t mkv_paged_workspace_bytes(int q_heads, int kv_heads, int head_dim, int max_batch) {
+    if (q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || q_heads / kv_heads > kPagedMaxGroup) return 0;
+    if (!shape_ok(kv_heads, head_dim, 16, MKV_BF16) || max_batch < 1 || max_batch > 65535) return 0;
+    return paged_ws().total;
+}
+
+mkv_status mkv_paged_create(int layers, int q_heads, int kv_heads, int head_dim, int page_size, int n_pages,
+                            int max_batch, int kv_dtype, int io_dtype, int out_dtype, void* pages, size_t pages_bytes,
+                            void* workspace, size_t workspace_bytes, int device, mkv_paged** out) {
+    if (!out) return MKV_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (layers < 1 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || n_pages < 1) return MKV_ERR_INVALID_ARG;
+    if (max_batch < 1 || max_batch > 65535 || device < 0 || !pages || !workspace) return MKV_ERR_INVALID_ARG;
+    if (kv_dtype != MKV_BF16 && kv_dtype != MKV_F32 && kv_dtype != MKV_INT4) return MKV_ERR_INVALID_ARG;
+    if ((io_dtype != MKV_BF16 && io_dtype != MKV_F32) || (out_dtype != MKV_BF16 && out_dtype != MKV_F32))
+        return MKV_ERR_INVALID_ARG;
+    if (kv_dtype != MKV_INT4 && io_dtype != kv_dtype) return MKV_ERR_INVALID_ARG;
+    if (io_dtype == MKV_F32 && out_dtype != MKV_F32) return MKV_ERR_INVALID_ARG;
+    if (!shape_ok(kv_heads, head_dim, page_size, kv_dtype) || q_heads / kv_heads > kPagedMaxGroup) return MKV_ERR_UNSUPPORTED;
+    const size_t page = mkv_paged_page_bytes(kv_heads, head_dim, page_size, kv_dtype);
+    if (!aligned16(pages) || pages_bytes / page / (size_t)n_pages < (size_t)layers) return MKV_ERR_INVALID_ARG;
+    if (((uintptr_t)workspace & 255u) || workspace_bytes < mkv_paged_workspace_bytes(q_heads, kv_heads, head_dim, max_batch))
+        return MKV_ERR_WORKSPACE;
+    DeviceGuard guard(device);
+    if (!guard.ok) return MKV_ERR_CUDA;
+    mkv_paged* c = new (std::nothrow) mkv_paged();
+    if (!c) return MKV_ERR_INVALID_ARG;
+    c->layers = layers; c->q_heads = q_heads; c->kv_heads = kv_heads; c->head_dim = head_dim;
+    c->page_size = page_size; c->n_pages = n_pages; c->max_batch = max_batch;
+    c->kv_dtype = kv_dtype; c->io_dtype = io_dtype; c->out_dtype = out_dtype; c->device = device;
+    c->pages = (uint8_t*)pages; c->ws = (uint8_t*)workspace;
+    c->rot_dim = 0; c->interleaved = 0; c->launches = 0;
+    if (cudaMemset(workspace, 0, paged_ws().total) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+        delete c;
+        return MKV_ERR_CUDA;
+    }
+    *out = c;
+    return MKV_OK;
+}
+
+void mkv_paged_destroy(mkv_paged* c) { delete c; }
+
+mkv_status mkv_paged_set_rotation(mkv_paged* c, const float* inv_freq, int rot_dim, int style) {
+    if (!c || rot_dim < 0 || rot_dim > c->head_dim || (rot_dim > 0 && !inv_freq)) return MKV_ERR_INVALID_ARG;
+    if (style != MKV_ROTATE_HALVES && style != MKV_ROTATE_NEIGHBOURS) return MKV_ERR_INVALID_ARG;
+    if (rot_dim % 16) return MKV_ERR_UNSUPPORTED;
+    DeviceGuard guard(c->device);
+    if (!guard.ok || cudaDeviceSynchronize() != cudaSuccess) return MKV_ERR_CUDA;
+    if (rot_dim > 0 && cudaMemcpy(c->ws + paged_ws().inv_freq, inv_freq, (size_t)rot_dim / 2 * 4, cudaMemcpyHostToDevice) != cudaSuccess)
+        return MKV_ERR_CUDA;
+    c->rot_dim = rot_dim;
+    c->interleaved = style == MKV_ROTATE_NEIGHBOURS;
+    return MKV_OK;
+}
+
+mkv_status mkv_paged_append(mkv_paged* c, int layer, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                            const void* v, int64_t v_stride, void* q_out, int n_tokens, int batch,
+                            const int32_t* starts, const int32_t* lens, const int32_t* table, int table_stride,
+                            const int32_t* positions, void* stream) {
+    const mkv_status s = batch_args(c, layer, n_tokens, batch, starts, lens, table, table_stride);
+    if (s != MKV_OK) return s;
+    if (n_tokens == 0) return MKV_OK;
+    if (!strided_ok(c, k, k_stride, c->kv_heads) || !strided_ok(c, v, v_stride, c->kv_heads)) return MKV_ERR_INVALID_ARG;
+    if ((q != nullptr) != (q_out != nullptr)) return MKV_ERR_INVALID_ARG;
+    if (q && (!strided_ok(c, q, q_stride, c->q_heads) || !aligned16(q_out))) return MKV_ERR_INVALID_ARG;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return MKV_ERR_CUDA;
+    PagedAppendArgs a;
+    a.c = dev_of(c, layer);
+    a.b = {starts, lens, table, n_tokens, batch, table_stride};
+    a.q = q; a.k = k; a.v = v; a.q_out = q_out;
+    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+    a.positions = positions;
+    a.inv_freq = (const float*)(c->ws + paged_ws().inv_freq);
+    a.rot_dim = c->rot_dim; a.interleaved = c->interleaved;
+    if (launch_paged_append(a, c->head_dim, (cudaStream_t)stream) != cudaSuccess) return MKV_ERR_CUDA;
+    c->launches += 1;
+    return MKV_OK;
+}
+
+mkv_status mkv_paged_attend(mkv_paged* c, int layer, const void* q, int64_t q_stride, void* out, float* lse,
+                            int n_tokens, int batch, const int32_t* starts, int max_new, const int32_t* lens,
+                            const int32_t* table, int table_stride, float scale, int window, void* stream) {
+    const mkv_status s = batch_args(c, layer, n_tokens, batch, starts, lens, table, table_stride);
+    if (s != MKV_OK) return s;
+    if (window < 0 || max_new < 1 || !(scale >= 0.0f) || !std::isfinite(scale)) return MKV_ERR_INVALID_ARG;
+    if (n_tokens == 0) return MKV_OK;
+    if (!strided_ok(c, q, q_stride, c->q_heads) || !out || !aligned16(out) || ((uintptr_t)lse & 3u)) return MKV_ERR_INVALID_ARG;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return MKV_ERR_CUDA;
+    PagedAttendArgs a;
+    a.c = dev_of(c, layer);
+    a.b = {starts, lens, table, n_tokens, batch, table_stride};
+    a.q = q; a.q_stride = q_stride; a.out = out; a.lse = lse;
+    a.max_new = starts ? max_new : 1;
+    a.window = window;
+    a.scale_log2 = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)c->head_dim)));
+    a.scratch = c->ws + paged_ws().scratch;
+    if (launch_paged_simt(a, c->head_dim, (cudaStream_t)stream) != cudaSuccess) return MKV_ERR_CUDA;
+    c->launches += 1;
+    return MKV_OK;
+}
+
+mkv_status mkv_paged_read(mkv_paged* c, int layer, int batch, const int32_t* first, const int32_t* lens,
+                          const int32_t* table, int table_stride, void* K, void* V, int rows, void* stream) {
+    const mkv_status s = batch_args(c, layer, batch, batch, nullptr, lens, table, table_stride);
+    if (s != MKV_OK) return s;
+    if (rows < 0) return MKV_ERR_INVALID_ARG;
+    if (rows == 0 || batch == 0) return MKV_OK;
+    if (!K || !V || !aligned16(K) || !aligned16(V)) return MKV_ERR_INVALID_ARG;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return MKV_ERR_CUDA;
+    PagedReadArgs a;
+    a.c = dev_of(c, layer);
+    a.b = {nullptr, lens, table, batch, batch, table_stride};
+    a.first = first; a.K = K; a.V = V; a.rows = rows;
+    if (launch_paged_read(a, c->head_dim, (cudaStream_t)stream) != cudaSuccess) return MKV_ERR_CUDA;
+    c->launches += 1;
+    return MKV_OK;
+}
+
+mkv_status mkv_paged_status_sync(mkv_paged* c, void* stream) {
+    if (!c) return MKV_ERR_INVALID_ARG;
+    DeviceGuard guard(c->device);
+    if (!guard.ok || cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return MKV_ERR_CUDA;
+    int32_t s = 0;
+    if (cudaMemcpy(&s, c->ws + paged_ws().status, 4, cudaMemcpyDeviceToHost) != cudaSuccess) return MKV_ERR_CUDA;
+    return (mkv_status)s;
+}
+
+mkv_status mkv_paged_reset(mkv_paged* c) {
+    if (!c) return MKV_ERR_INVALID_ARG;
+    DeviceGuard guard(c->device);
+    if (!guard.ok || cudaDeviceSynchronize() != cudaSuccess) return MKV_ERR_CUDA;
+    const PagedWs w = paged_ws();
+    if (cudaMemset(c->ws + w.status, 0, 4) != cudaSuccess) return MKV_ERR_CUDA;
+    if (w.total > w.scratch && cudaMemset(c->ws + w.scratch, 0, w.total - w.scratch) != cudaSuccess) return MKV_ERR_CUDA;
+    return MKV_OK;
+}
+
+int64_t mkv_paged_launch_count(const mkv_paged* c) { return c ? c->launches : 0; }
+
+}  // extern "C"

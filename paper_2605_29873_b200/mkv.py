@@ -9,12 +9,13 @@ import os
 
 import numpy as np
 
-MKV_BF16, MKV_F32 = 0, 1
+MKV_BF16, MKV_F32, MKV_INT4 = 0, 1, 2
 MKV_SCORE_GROUP_MEAN, MKV_SCORE_LAYER_MEAN = 0, 1
 MKV_KERNEL_AUTO, MKV_KERNEL_SIMT, MKV_KERNEL_MMA = 0, 1, 2
 MKV_FLAG_RECORD_PROBS, MKV_FLAG_INPUTS_READY, MKV_FLAG_REPRODUCIBLE = 1, 2, 4
 MKV_OPT_RING_STAGES, MKV_OPT_HEAD_TILES, MKV_OPT_WAIT_LIMIT_US, MKV_OPT_OVERLAP, MKV_OPT_GRID_SHARE = 1, 2, 3, 4, 5
 MKV_INJECT_LOST_TILE = 0
+MKV_ROTATE_HALVES, MKV_ROTATE_NEIGHBOURS = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmkv.so")
@@ -26,6 +27,9 @@ EXPORTED_SYMBOLS = [
     "mkv_get_last_probs", "mkv_read_kv", "mkv_get_step", "mkv_status_string", "mkv_attend_noalloc", "mkv_plan_starts", "mkv_prefill_units",
     "mkv_recency_diagnostics", "mkv_set_option", "mkv_plan_ranges", "mkv_grid_limit", "mkv_decode_step_layers",
     "mkv_attend_only_layers", "mkv_get_grid", "mkv_debug_inject",
+    "mkv_paged_page_bytes", "mkv_paged_workspace_bytes", "mkv_paged_create", "mkv_paged_destroy", "mkv_paged_set_rotation",
+    "mkv_paged_append", "mkv_paged_attend", "mkv_paged_read", "mkv_paged_status_sync", "mkv_paged_reset",
+    "mkv_paged_launch_count",
 ]
 
 
@@ -82,6 +86,23 @@ def load_library(path: str | None = None):
     L.mkv_attend_only_layers.argtypes = [vp, C.c_int, C.c_int, vp, vp, vp]
     L.mkv_get_grid.argtypes = [vp, C.c_int, i32p, i32p]
     L.mkv_debug_inject.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_int]
+    i64 = C.c_int64
+    L.mkv_paged_page_bytes.restype = C.c_size_t
+    L.mkv_paged_page_bytes.argtypes = [C.c_int] * 4
+    L.mkv_paged_workspace_bytes.restype = C.c_size_t
+    L.mkv_paged_workspace_bytes.argtypes = [C.c_int] * 4
+    L.mkv_paged_create.argtypes = [C.c_int] * 10 + [vp, C.c_size_t, vp, C.c_size_t, C.c_int, C.POINTER(vp)]
+    L.mkv_paged_destroy.restype = None
+    L.mkv_paged_destroy.argtypes = [vp]
+    L.mkv_paged_set_rotation.argtypes = [vp, f32p, C.c_int, C.c_int]
+    L.mkv_paged_append.argtypes = [vp, C.c_int, vp, i64, vp, i64, vp, i64, vp, C.c_int, C.c_int, vp, vp, vp, C.c_int, vp, vp]
+    L.mkv_paged_attend.argtypes = [vp, C.c_int, vp, i64, vp, vp, C.c_int, C.c_int, vp, C.c_int, vp, vp, C.c_int, C.c_float,
+                                   C.c_int, vp]
+    L.mkv_paged_read.argtypes = [vp, C.c_int, C.c_int, vp, vp, vp, C.c_int, vp, vp, C.c_int, vp]
+    L.mkv_paged_status_sync.argtypes = [vp, vp]
+    L.mkv_paged_reset.argtypes = [vp]
+    L.mkv_paged_launch_count.restype = i64
+    L.mkv_paged_launch_count.argtypes = [vp]
     L.mkv_status_string.restype = C.c_char_p
     L.mkv_status_string.argtypes = [C.c_int]
     if path is None:
@@ -350,3 +371,154 @@ class MomentKV:
     def budget_cap(self) -> int:
         """Rows per decode pool: the largest budget plus the fresh token's slot."""
         return self.budget_max + 1
+
+
+def paged_page_bytes(kv_heads, head_dim, page_size, kv_dtype=MKV_BF16) -> int:
+    return int(load_library().mkv_paged_page_bytes(kv_heads, head_dim, page_size, kv_dtype))
+
+
+def paged_workspace_bytes(q_heads, kv_heads, head_dim, max_batch) -> int:
+    return int(load_library().mkv_paged_workspace_bytes(q_heads, kv_heads, head_dim, max_batch))
+
+
+class PagedKV:
+    """A handle on a paged cache (``mkv_paged_*``) and the torch tensor that backs its workspace.
+
+    ``pages`` is the caller's device tensor [layers, n_pages, ...]: bf16 or fp32
+    [layers, n_pages, 2, kv_heads, page_size, head_dim], or with ``MKV_INT4`` uint8
+    [layers, n_pages, kv_heads, page_size // 16 * block bytes] (``include/mkv.h`` has the layout).
+    ``lens`` [batch], ``table`` [batch, pages of a sequence] and ``starts`` [batch + 1] are int32
+    device tensors, see the header.  q, k and v are [tokens, heads, head_dim] with any distance
+    between tokens (slices of one projection's output)."""
+
+    def __init__(self, pages, q_heads, kv_heads, head_dim, page_size, max_batch, kv_dtype=MKV_BF16, io_dtype=None,
+                 out_dtype=None):
+        import torch
+
+        self._L = load_library()
+        self._ctx = C.c_void_p(0)
+        self.torch = torch
+        if not pages.is_cuda:
+            raise RuntimeError("PagedKV needs its pages on a CUDA device: there is no CPU implementation")
+        self.q_heads, self.kv_heads, self.head_dim, self.page_size = q_heads, kv_heads, head_dim, page_size
+        self.max_batch, self.kv_dtype = max_batch, kv_dtype
+        self.io_dtype = (MKV_F32 if kv_dtype == MKV_F32 else MKV_BF16) if io_dtype is None else io_dtype
+        self.out_dtype = self.io_dtype if out_dtype is None else out_dtype
+        self.device, self.pages = pages.device, pages
+        self._io, self._out = (torch.bfloat16 if t == MKV_BF16 else torch.float32 for t in (self.io_dtype, self.out_dtype))
+        page = paged_page_bytes(kv_heads, head_dim, page_size, kv_dtype)
+        nbytes = paged_workspace_bytes(q_heads, kv_heads, head_dim, max_batch)
+        if page == 0 or nbytes == 0:
+            raise MkvError(5, "PagedKV")
+        want = {MKV_BF16: torch.bfloat16, MKV_F32: torch.float32}.get(kv_dtype, torch.uint8)
+        assert pages.is_contiguous() and pages.dtype == want and pages.dim() >= 3
+        self.layers, self.n_pages = int(pages.shape[0]), int(pages.shape[1])
+        size = pages.numel() * pages.element_size()
+        assert size == self.layers * self.n_pages * page, "pages: not [layers, n_pages] pages of this shape"
+        self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        off = (-self.workspace.data_ptr()) % 256
+        torch.cuda.synchronize(self.device)
+        ctx = C.c_void_p(0)
+        index = torch.cuda.current_device() if self.device.index is None else self.device.index
+        _check(self._L.mkv_paged_create(self.layers, q_heads, kv_heads, head_dim, page_size, self.n_pages, max_batch, kv_dtype,
+                                        self.io_dtype, self.out_dtype, _ptr(pages), size,
+                                        C.c_void_p(self.workspace.data_ptr() + off), nbytes, index, C.byref(ctx)),
+               "mkv_paged_create")
+        self._ctx = ctx
+
+    def close(self):
+        if getattr(self, "_ctx", None) is not None and self._ctx.value:
+            self._L.mkv_paged_destroy(self._ctx)
+            self._ctx = C.c_void_p(0)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _stream(self, stream):
+        return (self.torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream
+
+    def _rows(self, x, heads):
+        """Pointer of [tokens, heads, head_dim] and the elements from one token to the next."""
+        n, h, d = x.shape
+        a, b, c = x.stride()
+        if h != heads or d != self.head_dim or x.dtype != self._io or x.device != self.device:
+            raise ValueError(f"expected [tokens, {heads}, {self.head_dim}] {self._io} on {self.device}, got {tuple(x.shape)} {x.dtype} on {x.device}")
+        if (d > 1 and c != 1) or (h > 1 and b != d):
+            raise ValueError("heads and channels of a token must be contiguous")
+        return x.data_ptr(), (a if n > 1 else heads * d)
+
+    def _batch(self, n_tokens, lens, table, starts):
+        batch, i32 = lens.shape[0], self.torch.int32
+        if lens.dtype != i32 or table.dtype != i32 or lens.device != self.device or table.device != self.device:
+            raise ValueError("lens and table are int32 tensors of the cache's device")
+        if table.dim() != 2 or table.shape[0] != batch or table.stride(1) != 1 or not lens.is_contiguous():
+            raise ValueError("table is [batch, pages], its rows contiguous")
+        if starts is not None:
+            if starts.dtype != i32 or starts.device != self.device or starts.shape != (batch + 1,) or not starts.is_contiguous():
+                raise ValueError("starts is an int32 [batch + 1] tensor of the cache's device")
+        elif n_tokens != batch:
+            raise ValueError("without starts there is one new token per sequence")
+        return batch, lens.data_ptr(), table.data_ptr(), (table.stride(0) if batch > 1 else table.shape[1]), \
+            (starts.data_ptr() if starts is not None else None)
+
+    def _dense(self, x, shape, dtype):
+        if tuple(x.shape) != shape or x.dtype != dtype or x.device != self.device or not x.is_contiguous():
+            raise ValueError(f"expected a contiguous {shape} {dtype} tensor on {self.device}, got {tuple(x.shape)} {x.dtype} on {x.device}")
+        return x.data_ptr()
+
+    def set_rotation(self, inv_freq, interleaved=False):
+        """inv_freq: rot_dim / 2 numbers (a tensor or a sequence); empty = no rotation."""
+        f = np.ascontiguousarray(inv_freq.detach().cpu().numpy() if hasattr(inv_freq, "detach") else inv_freq, dtype=np.float32)
+        style = MKV_ROTATE_NEIGHBOURS if interleaved else MKV_ROTATE_HALVES
+        _check(self._L.mkv_paged_set_rotation(self._ctx, f.ctypes.data_as(C.POINTER(C.c_float)), 2 * f.size, style),
+               "mkv_paged_set_rotation")
+
+    def append(self, layer, q, k, v, lens, table, q_out=None, starts=None, positions=None, stream=None):
+        """Stores k (rotated) and v, writes the rotated q to q_out; q and q_out may both be None."""
+        n = k.shape[0]
+        qp, qs = self._rows(q, self.q_heads) if q is not None else (None, 0)
+        kp, ks = self._rows(k, self.kv_heads)
+        vp, vs = self._rows(v, self.kv_heads)
+        if v.shape[0] != n or (q is not None and q.shape[0] != n):
+            raise ValueError("q, k and v have the same tokens")
+        op = self._dense(q_out, (n, self.q_heads, self.head_dim), self._io) if q_out is not None else None
+        pos = self._dense(positions, (n,), self.torch.int32) if positions is not None else None
+        batch, lp, tp, stride, sp = self._batch(n, lens, table, starts)
+        rc = self._L.mkv_paged_append(self._ctx, layer, qp, qs, kp, ks, vp, vs, op, n, batch, sp, lp, tp, stride, pos,
+                                      self._stream(stream))
+        if rc:
+            raise MkvError(rc, "mkv_paged_append")
+
+    def attend(self, layer, q, lens, table, out, starts=None, max_new=1, scale=0.0, window=0, lse=None, stream=None):
+        n = q.shape[0]
+        qp, qs = self._rows(q, self.q_heads)
+        op = self._dense(out, (n, self.q_heads, self.head_dim), self._out)
+        ep = self._dense(lse, (n, self.q_heads), self.torch.float32) if lse is not None else None
+        batch, lp, tp, stride, sp = self._batch(n, lens, table, starts)
+        rc = self._L.mkv_paged_attend(self._ctx, layer, qp, qs, op, ep, n, batch, sp, max_new, lp, tp, stride, scale, window,
+                                      self._stream(stream))
+        if rc:
+            raise MkvError(rc, "mkv_paged_attend")
+
+    def read(self, layer, lens, table, K, V, first=None, stream=None):
+        """K, V [batch, kv_heads, rows, head_dim] receive the rows of positions [first, lens)."""
+        batch, lp, tp, stride, _ = self._batch(lens.shape[0], lens, table, None)
+        rows = K.shape[2]
+        shape = (batch, self.kv_heads, rows, self.head_dim)
+        kp, vp = self._dense(K, shape, self._io), self._dense(V, shape, self._io)
+        fp = self._dense(first, (batch,), self.torch.int32) if first is not None else None
+        rc = self._L.mkv_paged_read(self._ctx, layer, batch, fp, lp, tp, stride, kp, vp, rows, self._stream(stream))
+        if rc:
+            raise MkvError(rc, "mkv_paged_read")
+
+    def status_sync(self, stream=None):
+        _check(self._L.mkv_paged_status_sync(self._ctx, self._stream(stream)), "mkv_paged_status_sync")
+
+    def reset(self):
+        _check(self._L.mkv_paged_reset(self._ctx), "mkv_paged_reset")
+
+    def launch_count(self) -> int:
+        return int(self._L.mkv_paged_launch_count(self._ctx))
