@@ -1,4 +1,5 @@
 // C ABI of the paged cache: argument checks, workspace, launches.
+#include <cuda.h>
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -13,6 +14,8 @@ struct mkv_paged {
     uint8_t *pages, *ws;
     int rot_dim, interleaved;
     int64_t launches;
+    int sm_count;
+    alignas(64) CUtensorMap map;   // bf16: all pages as rows of head_dim
 };
 
 namespace {
@@ -23,7 +26,7 @@ PagedWs paged_ws() {
     w.status = 0;
     w.inv_freq = 256;
     w.scratch = 512;
-    w.total = w.scratch;
+    w.total = (w.scratch + paged_decode_scratch() + 255) / 256 * 256;
     return w;
 }
 
@@ -110,6 +113,8 @@ mkv_status mkv_paged_create(int layers, int q_heads, int kv_heads, int head_dim,
     if (kv_dtype != MKV_INT4 && io_dtype != kv_dtype) return MKV_ERR_INVALID_ARG;
     if (io_dtype == MKV_F32 && out_dtype != MKV_F32) return MKV_ERR_INVALID_ARG;
     if (!shape_ok(kv_heads, head_dim, page_size, kv_dtype) || q_heads / kv_heads > kPagedMaxGroup) return MKV_ERR_UNSUPPORTED;
+    // rows of all pages are numbered with 31 bits
+    if (kv_dtype == MKV_BF16 && (long long)layers * n_pages > (1ll << 31) / (2ll * kv_heads * page_size)) return MKV_ERR_UNSUPPORTED;
     const size_t page = mkv_paged_page_bytes(kv_heads, head_dim, page_size, kv_dtype);
     if (!aligned16(pages) || pages_bytes / page / (size_t)n_pages < (size_t)layers) return MKV_ERR_INVALID_ARG;
     if (((uintptr_t)workspace & 255u) || workspace_bytes < mkv_paged_workspace_bytes(q_heads, kv_heads, head_dim, max_batch))
@@ -123,6 +128,11 @@ mkv_status mkv_paged_create(int layers, int q_heads, int kv_heads, int head_dim,
     c->kv_dtype = kv_dtype; c->io_dtype = io_dtype; c->out_dtype = out_dtype; c->device = device;
     c->pages = (uint8_t*)pages; c->ws = (uint8_t*)workspace;
     c->rot_dim = 0; c->interleaved = 0; c->launches = 0;
+    if (cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
+        (kv_dtype == MKV_BF16 && !make_paged_map(&c->map, pages, (long long)layers * n_pages * 2 * kv_heads * page_size, head_dim))) {
+        delete c;
+        return MKV_ERR_CUDA;
+    }
     if (cudaMemset(workspace, 0, paged_ws().total) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
         delete c;
         return MKV_ERR_CUDA;
@@ -189,7 +199,11 @@ mkv_status mkv_paged_attend(mkv_paged* c, int layer, const void* q, int64_t q_st
     a.window = window;
     a.scale_log2 = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)c->head_dim)));
     a.scratch = c->ws + paged_ws().scratch;
-    if (launch_paged_simt(a, c->head_dim, (cudaStream_t)stream) != cudaSuccess) return MKV_ERR_CUDA;
+    const long long rows_per_layer = (long long)c->n_pages * 2 * c->kv_heads * c->page_size;
+    const cudaError_t e = c->kv_dtype != MKV_F32 && (long long)a.c.group * a.max_new <= 64
+                              ? launch_paged_decode(a, c->head_dim, &c->map, layer * rows_per_layer, c->sm_count, (cudaStream_t)stream)
+                              : launch_paged_simt(a, c->head_dim, (cudaStream_t)stream);
+    if (e != cudaSuccess) return MKV_ERR_CUDA;
     c->launches += 1;
     return MKV_OK;
 }

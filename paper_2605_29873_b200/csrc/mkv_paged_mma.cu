@@ -1,0 +1,923 @@
+// Attention over the paged cache for few rows (new tokens x query heads of a KV head): the cache is
+// streamed once, so the bound is HBM over bf16 pages and instruction issue over 4-bit pages.
+//
+// Work.  A unit is one (sequence, KV head, tile of RT rows); its cache rows are blocks of 16 tokens.
+// All units' blocks form one list (sequence, head, row tile, block), cut into one contiguous range
+// per CTA, so CTAs get equal shares whatever the lengths, and the cut depends on nothing but the
+// lengths: the same inputs give the same bits.  Lengths are on the device; every CTA sums them for
+// itself.  The warps of a CTA take the blocks of a unit in turn, each with its own online softmax
+// (m, l, O) and its own ring of shared-memory stages that its lane 0 fills by bulk copies, several
+// blocks ahead and across unit borders; nothing but the end of a unit makes the warps meet.  There
+// they add up their states.  A unit cut by range borders leaves its parts in the workspace, and the
+// CTA that delivers the last of them joins them in the order of the ranges.
+//
+// Per block and warp, rows in M, tokens in N:
+//   S[16 rows x 8 tokens] = Q K^T                    two tiles of eight tokens
+//   p = 2^(s - m), m moved only when a logit exceeds it by 2^8 (every row's weights stay within fp32
+//   and what is left out is exact: m is a reference, not the maximum)
+//   O^T[16 channels x 8 rows] += V^T P^T             the first product's accumulators are, register for
+//                                                    register, the second's operand
+// bf16 pages: rows arrive by 2D bulk tensor copies with the 128-byte swizzle that ldmatrix reads
+// without conflicts.  P enters as the sum of two bf16 (2^-17 of it is left).
+//
+// 4-bit pages: a nibble under a mask is an fp16 subnormal, n * 2^-24 (low) or n * 2^-20 (second), exact
+// in the matrix units, so eight codes become operands with five instructions and no conversion:
+//   s = sum_g scale_g (q . codes)_g + lowest_g * sum(q)_g   products per group of 32 channels, the scale
+//       applied to their fp32 sums, the second term one more matrix product with sum(q) as three bf16
+//   O = sum_t codes_t (p_t scale_t) + lowest_t p_t          p * scale in fp16 per group; lowest again
+//       one more product, p as two bf16
+// q enters as fp16 scaled by a power of two to the top of its range: exact for bf16 queries down to
+// 2^-24 of a row's largest; fp32 queries as a sum of two fp16 in the unused half of the 16 rows.
+// p * scale is kept within fp16 by moving m with log2 of the block's largest scale: rounding 2^-12 of
+// each weight, below what a bf16 result shows; with fp32 results it enters as the sum of two fp16.
+#include <cuda.h>
+#include <cuda_fp16.h>
+#include <cfloat>
+#include <climits>
+#include <type_traits>
+
+#include "mkv_paged.cuh"
+#include "mkv_ptx.cuh"
+
+namespace mkv {
+namespace {
+
+constexpr int kW = 8;                       // warps of a CTA
+constexpr int kThreads = kW * 32;
+constexpr unsigned long long kWaitNs = 2000000000ull;
+constexpr int kMaxParts = 64;               // ranges that may share one unit
+constexpr unsigned kFull = 0xffffffffu;
+
+template <int KIND, int D, int NT>
+struct Cfg {
+    static constexpr int RT = 8 * NT;
+    static constexpr int kStage = KIND == MKV_INT4 ? 16 * D + 128 * (D / 32) : 16 * D * 4;
+    // bytes in flight per SM want 44 KB (6.5 TB/s x 1 us / 148): three stages of eight warps, of which one is read
+    static constexpr int kStages = KIND == MKV_INT4 || NT == 1 ? 3 : 2;
+    static constexpr int DP = D + 4;
+    static constexpr int kRing = kW * kStages * kStage;
+    static constexpr int kMerge = kW * RT * DP * 4;
+    static constexpr int kMl = kW * RT * 8;
+    static constexpr int kSmem = 1024 + kRing + kMerge + kMl;
+};
+
+__device__ inline float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ inline void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ inline uint32_t pack_f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ inline float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ inline float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ inline float2 f16x2_floats(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+template <int N> struct Words { uint32_t w[N]; };
+template <int N> __device__ inline Words<N> lds_words(uint32_t addr) {
+    Words<N> r;
+    if (N == 4) asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[N > 2 ? 2 : 0]), "=r"(r.w[N > 2 ? 3 : 0]) : "r"(addr));
+    else asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r.w[0]), "=r"(r.w[1]) : "r"(addr));
+    return r;
+}
+__device__ inline uint32_t lds32(uint32_t addr) {
+    uint32_t r;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r) : "r"(addr));
+    return r;
+}
+__device__ inline void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
+// One (sequence, KV head, row tile), and the part of the block list that is its own.
+struct Unit {
+    long long base;   // of its first block in the list
+    int s, h, rt;
+    int tok0, n, len;
+    int row0, rows;   // rows [row0, row0 + rows) of the n * group of its sequence and head
+    int plo, phi;     // positions of the first and the last row's token
+    int blk0, nblk;   // blocks to read; a unit without any counts as one in the list
+    __device__ int count() const { return max(nblk, 1); }
+    __device__ long long end() const { return base + count(); }
+};
+
+template <int RT>
+__device__ inline void unit_rows(const PagedAttendArgs& a, Unit& u) {
+    const int G = a.c.group, R = u.n * G;
+    u.row0 = u.rt * RT;
+    u.rows = min(RT, R - u.row0);
+    u.plo = u.len - u.n + u.row0 / G;
+    u.phi = u.len - u.n + (u.row0 + u.rows - 1) / G;
+    const int begin = a.window > 0 ? max(0, u.plo - a.window + 1) : 0;
+    u.blk0 = begin >> 4;
+    u.nblk = u.phi >= begin ? (u.phi >> 4) - u.blk0 + 1 : 0;
+}
+template <int RT> __device__ inline int row_tiles(const PagedAttendArgs& a, int n) { return (n * a.c.group + RT - 1) / RT; }
+
+// Blocks of one head of sequence s in the list.
+template <int RT>
+__device__ inline long long blocks_per_head(const PagedAttendArgs& a, const PagedSpan& sp) {
+    Unit u;
+    u.n = sp.n; u.len = sp.len;
+    long long t = 0;
+    const int rts = row_tiles<RT>(a, sp.n);
+    for (u.rt = 0; u.rt < rts; ++u.rt) { unit_rows<RT>(a, u); t += u.count(); }
+    return t;
+}
+
+// Moves u to the next unit that has rows; false behind the last.
+template <int RT>
+__device__ inline bool next_unit(const PagedAttendArgs& a, Unit& u) {
+    u.base = u.end();
+    if (++u.rt >= row_tiles<RT>(a, u.n)) {
+        u.rt = 0;
+        if (++u.h >= a.c.kv_heads) {
+            u.h = 0;
+            do {
+                if (++u.s >= a.b.batch) return false;
+                const PagedSpan sp = paged_span(a.c, a.b, u.s);
+                u.tok0 = sp.tok0; u.n = sp.n; u.len = sp.len;
+            } while (u.n == 0);
+        }
+    }
+    unit_rows<RT>(a, u);
+    return true;
+}
+
+struct Part { float *o, *m, *l; };
+// Part `slot` of the workspace: O [RT][D], m [RT], l [RT]
+template <int RT, int D>
+__device__ inline Part part_at(const PagedAttendArgs& a, int slot) {
+    float* p = reinterpret_cast<float*>(a.scratch + kPagedTickets * 4) + (size_t)slot * RT * (D + 2);
+    return {p, p + RT * D, p + RT * D + RT};
+}
+
+template <int D>
+__device__ inline void store_row(const PagedAttendArgs& a, const Unit& u, int row, int c, float4 o, float m, float l) {
+    const int r = u.row0 + row, j = r / a.c.group, h = u.h * a.c.group + (r - j * a.c.group);
+    const size_t at = (size_t)(u.tok0 + j) * a.c.q_heads + h;
+    // l is 0 where nothing was seen and NaN where a NaN was
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (a.c.out_f32) {
+        *reinterpret_cast<float4*>((float*)a.out + at * D + c) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    } else {
+        uint2 w;
+        w.x = ptx::pack_bf16x2(o.x * inv, o.y * inv);
+        w.y = ptx::pack_bf16x2(o.z * inv, o.w * inv);
+        *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + at * D + c) = w;
+    }
+    if (a.lse && c == 0) a.lse[at] = l == 0.f ? kPagedNegInf : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+// A warp's state over the blocks it has worked through.
+template <int D, int NT>
+struct State {
+    float m[NT], l[NT];         // row g (+ 8): reference and this lane's share of the sum
+    float o[D / 16][NT][4];     // channels x rows
+    float lowest[NT][4];        // 4 bits: groups x rows
+};
+
+// m of the rows that a lane's columns of O belong to, after a move of the reference by `sc`
+template <int D, int NT>
+__device__ inline void rescale(State<D, NT>& st, const float (&sc)[NT], int lane) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        st.l[n] *= sc[n];
+        const float s0 = __shfl_sync(kFull, sc[n], (lane & 3) * 8), s1 = __shfl_sync(kFull, sc[n], (lane & 3) * 8 + 4);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            st.o[i][n][0] *= s0; st.o[i][n][1] *= s1; st.o[i][n][2] *= s0; st.o[i][n][3] *= s1;
+        }
+        st.lowest[n][0] *= s0; st.lowest[n][1] *= s1;
+    }
+}
+
+// The softmax step of a block: s[token tile][..] in, p out.  What p will be multiplied by: token (x, e) of
+// the lane by 2^lv_of(x, e), no token of the lane by more than 2^lv.  The reference m moves when a
+// product could exceed 2^room; the largest is then 2^head.
+// EDGE: not every row sees every token of the block.
+template <int D, int NT, bool EDGE, typename LvOf>
+__device__ inline void softmax_step(State<D, NT>& st, float (&s)[2][4], const int (&pos)[NT], int window, int tok, float lv,
+                                    float room, float head, int lane, LvOf lv_of) {
+    // element (tile x, e) of row n: s[x][2 n + e], token tok + 8 x + 2 t + e
+    const int t2 = tok + 2 * (lane & 3);
+    if (EDGE) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int hi = pos[n] - t2, lo = window > 0 ? hi - window : INT_MIN;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (8 * x + e > hi || 8 * x + e <= lo) s[x][2 * n + e] = kPagedNegInf;
+        }
+    }
+    bool move = false;
+    float mx[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        mx[n] = fmaxf(fmaxf(s[0][2 * n], s[0][2 * n + 1]), fmaxf(s[1][2 * n], s[1][2 * n + 1])) + lv;
+        move |= mx[n] > st.m[n] + room;
+    }
+    if (__any_sync(kFull, move)) {
+        float sc[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            // token by token now: the largest logit and the largest factor may be different tokens'
+            mx[n] = fmaxf(fmaxf(s[0][2 * n] + lv_of(0, 0), s[0][2 * n + 1] + lv_of(0, 1)),
+                          fmaxf(s[1][2 * n] + lv_of(1, 0), s[1][2 * n + 1] + lv_of(1, 1)));
+            mx[n] = fmaxf(mx[n], __shfl_xor_sync(kFull, mx[n], 1));
+            mx[n] = fmaxf(mx[n], __shfl_xor_sync(kFull, mx[n], 2));
+            const float m = fmaxf(st.m[n], mx[n] - head);
+            sc[n] = ex2(st.m[n] - m);
+            st.m[n] = m;
+        }
+        rescale<D, NT>(st, sc, lane);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float p = ex2(s[x][2 * n + e] - st.m[n]);
+                s[x][2 * n + e] = p;
+                st.l[n] += p;
+            }
+}
+
+// ---- bf16 pages
+
+template <int D, int NT>
+struct QBf16 { uint32_t a[D / 16][NT == 1 ? 2 : 4]; };
+
+template <int D, int NT>
+__device__ inline void load_q(const PagedAttendArgs& a, const Unit& u, QBf16<D, NT>& q, int lane) {
+    const int G = a.c.group, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int row = u.row0 + (lane >> 2) + 8 * n, j = row / G;
+        const bool live = (lane >> 2) + 8 * n < u.rows;
+        const __nv_bfloat16* p = (const __nv_bfloat16*)a.q + (size_t)(u.tok0 + j) * a.q_stride + (size_t)(u.h * G + row - j * G) * D + 2 * t;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            // operand order: (row g, k low), (row g + 8, k low), (row g, k high), (row g + 8, k high)
+            q.a[k][n] = live ? *reinterpret_cast<const uint32_t*>(p + 16 * k) : 0u;
+            q.a[k][NT + n] = live ? *reinterpret_cast<const uint32_t*>(p + 16 * k + 8) : 0u;
+        }
+    }
+}
+
+template <int D, int NT, bool EDGE>
+__device__ inline void block_bf16(State<D, NT>& st, const QBf16<D, NT>& q, const PagedAttendArgs& a, const Unit& u,
+                                  const int (&pos)[NT], uint32_t stage, int tok, int lane) {
+    // tiles of 16 rows x 64 channels, 128-byte rows, 16-byte chunk c of row r at c ^ (r & 7)
+    const int r = (lane & 7) + ((lane >> 4) << 3), c0 = (lane >> 3) & 1;
+    const uint32_t row = stage + r * 128;
+    float s[2][4] = {};
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+        uint32_t b0, b1, b2, b3;
+        ptx::ldmatrix_x4(row + (k >> 2) * 2048 + (((2 * (k & 3) + c0) ^ (r & 7)) << 4), b0, b1, b2, b3);
+        const uint32_t a0 = q.a[k][0], a1 = NT == 1 ? 0u : q.a[k][1], a2 = q.a[k][NT], a3 = NT == 1 ? 0u : q.a[k][2 * NT - 1];
+        ptx::mma_bf16(s[0], a0, a1, a2, a3, b0, b1);
+        ptx::mma_bf16(s[1], a0, a1, a2, a3, b2, b3);
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int e = 0; e < 2 * NT; ++e) s[x][e] *= a.scale_log2;
+    softmax_step<D, NT, EDGE>(st, s, pos, a.window, tok, 0.f, 8.f, 0.f, lane, [](int, int) { return 0.f; });
+    uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const float p0 = s[x][2 * n], p1 = s[x][2 * n + 1];
+            hi[n][x] = ptx::pack_bf16x2(p0, p1);
+            lo[n][x] = ptx::pack_bf16x2(p0 - lo_bf16(hi[n][x]), p1 - hi_bf16(hi[n][x]));
+        }
+    const uint32_t vrow = row + 16 * D * 2;
+    uint32_t keep0 = kFull, keep1 = kFull;
+    bool apart = false;
+    if (EDGE) {
+        // rows of V that no row of the tile sees may hold anything
+        const int first = a.window > 0 ? u.plo - a.window + 1 : 0, t2 = tok + 2 * (lane & 3);
+        auto in = [&](int x) { return x >= first && x <= u.phi ? 0xffffu : 0u; };
+        keep0 = in(t2) | in(t2 + 1) << 16;
+        keep1 = in(t2 + 8) | in(t2 + 9) << 16;
+        if (u.plo != u.phi) {
+            // one that some rows see and others do not must not meet the others' zero weights if it is not finite
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                uint32_t v[4];
+                ptx::ldmatrix_x4_trans(vrow + (i >> 2) * 2048 + (((2 * (i & 3) + c0) ^ (r & 7)) << 4), v[0], v[1], v[2], v[3]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t w = v[e] & (e < 2 ? keep0 : keep1);
+                    odd |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+                }
+            }
+            apart = __any_sync(kFull, odd);
+        }
+    }
+    if (EDGE && apart) {
+        // a product per new token, of which its own rows are kept
+        const int G = a.c.group, t = lane & 3;
+        for (int p = u.plo; p <= u.phi; ++p) {
+            const int first = a.window > 0 ? p - a.window + 1 : 0, t2 = tok + 2 * t;
+            auto in = [&](int x) { return x >= first && x <= p ? 0xffffu : 0u; };
+            const uint32_t k0 = in(t2) | in(t2 + 1) << 16, k1 = in(t2 + 8) | in(t2 + 9) << 16;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                uint32_t v[4];
+                ptx::ldmatrix_x4_trans(vrow + (i >> 2) * 2048 + (((2 * (i & 3) + c0) ^ (r & 7)) << 4), v[0], v[1], v[2], v[3]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float x[4] = {};
+                    ptx::mma_bf16(x, v[0] & k0, v[1] & k0, v[2] & k1, v[3] & k1, hi[n][0], hi[n][1]);
+                    ptx::mma_bf16(x, v[0] & k0, v[1] & k0, v[2] & k1, v[3] & k1, lo[n][0], lo[n][1]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int rr = u.row0 + 8 * n + 2 * t + (e & 1);
+                        if (u.len - u.n + rr / G == p) st.o[i][n][e] += x[e];
+                    }
+                }
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+        uint32_t v[4];
+        ptx::ldmatrix_x4_trans(vrow + (i >> 2) * 2048 + (((2 * (i & 3) + c0) ^ (r & 7)) << 4), v[0], v[1], v[2], v[3]);
+        if (EDGE) { v[0] &= keep0; v[1] &= keep0; v[2] &= keep1; v[3] &= keep1; }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            ptx::mma_bf16(st.o[i][n], v[0], v[1], v[2], v[3], hi[n][0], hi[n][1]);
+            ptx::mma_bf16(st.o[i][n], v[0], v[1], v[2], v[3], lo[n][0], lo[n][1]);
+        }
+    }
+}
+
+// ---- 4-bit pages
+
+// Q as fp16 scaled to the top of its range, in the channel order of the codes' words, and its group sums
+// as three bf16 along the k of one more product.  With Q32 rows 8..15 hold what is left of rows 0..7.
+template <int D, int NT, bool Q32>
+struct QInt4 {
+    uint32_t a[D / 16][NT == 1 && !Q32 ? 2 : 4];
+    uint32_t sum[NT][2];    // rows g (+ 8): k low, k high
+    float back[NT];         // scale * log2(e) * 2^(24 - e)
+};
+
+template <int D, int NT, bool Q32>
+__device__ inline void load_q(const PagedAttendArgs& a, const Unit& u, QInt4<D, NT, Q32>& q, int lane) {
+    constexpr int NG = D / 32;
+    const int G = a.c.group, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int row = u.row0 + (lane >> 2) + 8 * n, j = row / G;
+        const bool live = (lane >> 2) + 8 * n < u.rows;
+        const size_t at = (size_t)(u.tok0 + j) * a.q_stride + (size_t)(u.h * G + row - j * G) * D + 8 * t;
+        float x[NG][8];
+        float big = 0.f;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            if (!live) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[g][e] = 0.f;
+            } else if (Q32) {
+                const float4 v0 = *reinterpret_cast<const float4*>((const float*)a.q + at + 32 * g);
+                const float4 v1 = *reinterpret_cast<const float4*>((const float*)a.q + at + 32 * g + 4);
+                x[g][0] = v0.x; x[g][1] = v0.y; x[g][2] = v0.z; x[g][3] = v0.w;
+                x[g][4] = v1.x; x[g][5] = v1.y; x[g][6] = v1.z; x[g][7] = v1.w;
+            } else {
+                const uint4 v = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + at + 32 * g);
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { x[g][2 * e] = lo_bf16(w[e]); x[g][2 * e + 1] = hi_bf16(w[e]); }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(x[g][e]));
+        }
+        big = fmaxf(big, __shfl_xor_sync(kFull, big, 1));
+        big = fmaxf(big, __shfl_xor_sync(kFull, big, 2));
+        // exponent field of the largest; 2^e brings it to [2^13, 2^14).  Kept where 2^e and 2^-e are normal.
+        const int ex = min(max((int)(__float_as_uint(big) >> 23), 16), 254);
+        const float up = __uint_as_float((uint32_t)min(254, 127 + 13 + 127 - ex) << 23);
+        q.back[n] = a.scale_log2 * (1.f / up);   // times 2^24 below
+        float sums[NG];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { x[g][e] *= up; sum += x[g][e]; }
+            sum += __shfl_xor_sync(kFull, sum, 1);
+            sum += __shfl_xor_sync(kFull, sum, 2);
+            sums[g] = sum * 5.9604644775390625e-08f;   // 2^-24, as the codes are
+            // codes' word: nibbles (0, 4), (1, 5) x 16, (2, 6), (3, 7) x 16
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float y0 = x[g][2 * h], y1 = x[g][2 * h + 4], z0 = x[g][2 * h + 1] * 0.0625f, z1 = x[g][2 * h + 5] * 0.0625f;
+                const uint32_t y = pack_f16x2(y0, y1), z = pack_f16x2(z0, z1);
+                constexpr int kRows = NT == 1 && !Q32 ? 1 : 2;
+                q.a[2 * g + h][n] = y;
+                q.a[2 * g + h][kRows + n] = z;
+                if (Q32) {
+                    const float2 yf = f16x2_floats(y), zf = f16x2_floats(z);
+                    q.a[2 * g + h][1] = pack_f16x2(y0 - yf.x, y1 - yf.y);
+                    q.a[2 * g + h][kRows + 1] = pack_f16x2(z0 - zf.x, z1 - zf.y);
+                }
+            }
+        }
+        q.back[n] *= 16777216.f;
+        // k index: pairs of groups, high parts first, then middle and low parts.  D = 128: lanes t = 0, 1 hold
+        // the high parts (k 0..3) and in the upper k (8..11) the low parts, t = 2, 3 the middle parts.
+        float part[3][NG];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            float rest = sums[g];
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                part[i][g] = __bfloat162float(__float2bfloat16_rn(rest));
+                rest -= part[i][g];
+            }
+        }
+        if (NG == 4) {
+            const bool up2 = t & 1, mid = t >= 2;
+            const float h0 = mid ? (up2 ? part[1][NG - 2] : part[1][0]) : (up2 ? part[0][NG - 2] : part[0][0]);
+            const float h1 = mid ? (up2 ? part[1][NG - 1] : part[1][1]) : (up2 ? part[0][NG - 1] : part[0][1]);
+            q.sum[n][0] = ptx::pack_bf16x2(h0, h1);
+            q.sum[n][1] = mid ? 0u : ptx::pack_bf16x2(up2 ? part[2][NG - 2] : part[2][0], up2 ? part[2][NG - 1] : part[2][1]);
+        } else {
+            const int i = min(t, 2);
+            q.sum[n][0] = t == 3 ? 0u : ptx::pack_bf16x2(i == 0 ? part[0][0] : i == 1 ? part[1][0] : part[2][0],
+                                                         i == 0 ? part[0][1] : i == 1 ? part[1][1] : part[2][1]);
+            q.sum[n][1] = 0u;
+        }
+    }
+}
+
+template <int D, int NT, bool Q32, bool HL, bool EDGE>
+__device__ inline void block_int4(State<D, NT>& st, const QInt4<D, NT, Q32>& q, const PagedAttendArgs& a, const Unit& u,
+                                  const int (&pos)[NT], uint32_t stage, int tok, int lane) {
+    constexpr int NG = D / 32;
+    const int g = lane >> 2, t = lane & 3;
+    const uint32_t par = stage + 16 * D;
+    float s[2][4];
+    // lowest * sum(q) first
+    {
+        float x0[4] = {}, x1[4] = {};
+        const uint32_t at = par + 32 * NG + (NG == 4 ? (t & 1) * 4 : 0);
+        const uint32_t k0 = lds32(at + g * NG * 2), k1 = lds32(at + (g + 8) * NG * 2);
+        const uint32_t a1 = NT == 2 ? q.sum[NT - 1][0] : 0u, a3 = NT == 2 ? q.sum[NT - 1][1] : 0u;
+        ptx::mma_bf16(x0, q.sum[0][0], a1, q.sum[0][1], a3, k0, k0);
+        ptx::mma_bf16(x1, q.sum[0][0], a1, q.sum[0][1], a3, k1, k1);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { s[0][e] = x0[e]; s[1][e] = x1[e]; }
+    }
+    const Words<NG> kw0 = lds_words<NG>(stage + g * (D / 2) + t * (4 * NG));
+    const Words<NG> kw1 = lds_words<NG>(stage + (g + 8) * (D / 2) + t * (4 * NG));
+    const Words<NG> ks0 = lds_words<NG>(par + t * (4 * NG)), ks1 = lds_words<NG>(par + (t + 4) * (4 * NG));
+#pragma unroll
+    for (int j = 0; j < NG; ++j) {
+        float x0[4] = {}, x1[4] = {};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t w0 = h ? kw0.w[j] >> 8 : kw0.w[j], w1 = h ? kw1.w[j] >> 8 : kw1.w[j];
+            const uint32_t* qa = q.a[2 * j + h];
+            constexpr int kRows = NT == 1 && !Q32 ? 1 : 2;
+            const uint32_t a0 = qa[0], a1 = kRows == 2 ? qa[1] : 0u, a2 = qa[kRows], a3 = kRows == 2 ? qa[2 * kRows - 1] : 0u;
+            mma_f16(x0, a0, a1, a2, a3, w0 & 0x000f000fu, w0 & 0x00f000f0u);
+            mma_f16(x1, a0, a1, a2, a3, w1 & 0x000f000fu, w1 & 0x00f000f0u);
+        }
+        if (Q32) { x0[0] += x0[2]; x0[1] += x0[3]; x1[0] += x1[2]; x1[1] += x1[3]; }
+        const float f00 = lo_bf16(ks0.w[j]), f01 = hi_bf16(ks0.w[j]), f10 = lo_bf16(ks1.w[j]), f11 = hi_bf16(ks1.w[j]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            s[0][2 * n] = fmaf(f00, x0[2 * n], s[0][2 * n]);
+            s[0][2 * n + 1] = fmaf(f01, x0[2 * n + 1], s[0][2 * n + 1]);
+            s[1][2 * n] = fmaf(f10, x1[2 * n], s[1][2 * n]);
+            s[1][2 * n + 1] = fmaf(f11, x1[2 * n + 1], s[1][2 * n + 1]);
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) { s[x][2 * n] *= q.back[n]; s[x][2 * n + 1] *= q.back[n]; }
+
+    Words<NG> vs0 = lds_words<NG>(par + 64 * NG + t * (4 * NG)), vs1 = lds_words<NG>(par + 64 * NG + (t + 4) * (4 * NG));
+    uint32_t keep0 = kFull, keep1 = kFull;
+    if (EDGE) {
+        // tokens that no row of the tile sees may hold anything
+        const int first = a.window > 0 ? u.plo - a.window + 1 : 0, t2 = tok + 2 * t;
+        auto in = [&](int x) { return x >= first && x <= u.phi ? 0xffffu : 0u; };
+        keep0 = in(t2) | in(t2 + 1) << 16;
+        keep1 = in(t2 + 8) | in(t2 + 9) << 16;
+#pragma unroll
+        for (int j = 0; j < NG; ++j) { vs0.w[j] &= keep0; vs1.w[j] &= keep1; }
+    }
+    // log2 of the largest scale of this lane's tokens, rounded up (a NaN is passed over), kept where both p and
+    // p * scale are far from the ends of their ranges
+    auto log2_up = [](float x) { return x > 0.f ? (float)min(max((int)(__float_as_uint(x) >> 23) - 126, -88), 104) : -88.f; };
+    __nv_bfloat162 big0 = *(const __nv_bfloat162*)&vs0.w[0], big1 = *(const __nv_bfloat162*)&vs1.w[0];
+#pragma unroll
+    for (int j = 1; j < NG; ++j) {
+        big0 = __hmax2(big0, *(const __nv_bfloat162*)&vs0.w[j]);
+        big1 = __hmax2(big1, *(const __nv_bfloat162*)&vs1.w[j]);
+    }
+    const __nv_bfloat162 big = __hmax2(big0, big1);
+    softmax_step<D, NT, EDGE>(st, s, pos, a.window, tok, log2_up(fmaxf(__low2float(big), __high2float(big))), 12.f, 4.f, lane,
+                              [&](int x, int e) {
+                                  const __nv_bfloat162 y = x ? big1 : big0;
+                                  return log2_up(e ? __high2float(y) : __low2float(y));
+                              });
+
+    // lowest values: p as two bf16; rows of the operand beyond the groups repeat them and are not read
+    {
+        const uint32_t at = par + 96 * NG + (g & (NG - 1)) * 4;
+        uint32_t l0 = lds32(at + t * (4 * NG)), l1 = lds32(at + (t + 4) * (4 * NG));
+        if (EDGE) { l0 &= keep0; l1 &= keep1; }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const uint32_t h0 = ptx::pack_bf16x2(s[0][2 * n], s[0][2 * n + 1]), h1 = ptx::pack_bf16x2(s[1][2 * n], s[1][2 * n + 1]);
+            const uint32_t r0 = ptx::pack_bf16x2(s[0][2 * n] - lo_bf16(h0), s[0][2 * n + 1] - hi_bf16(h0));
+            const uint32_t r1 = ptx::pack_bf16x2(s[1][2 * n] - lo_bf16(h1), s[1][2 * n + 1] - hi_bf16(h1));
+            ptx::mma_bf16(st.lowest[n], l0, 0u, l1, 0u, h0, h1);
+            ptx::mma_bf16(st.lowest[n], l0, 0u, l1, 0u, r0, r1);
+        }
+    }
+    const Words<NG> vw0 = lds_words<NG>(stage + 8 * D + t * D + g * (4 * NG)), vw1 = lds_words<NG>(stage + 8 * D + (t + 4) * D + g * (4 * NG));
+#pragma unroll
+    for (int j = 0; j < NG; ++j) {
+        const float f00 = lo_bf16(vs0.w[j]), f01 = hi_bf16(vs0.w[j]), f10 = lo_bf16(vs1.w[j]), f11 = hi_bf16(vs1.w[j]);
+        uint32_t b[NT][2], bl[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float y[4] = {s[0][2 * n] * f00, s[0][2 * n + 1] * f01, s[1][2 * n] * f10, s[1][2 * n + 1] * f11};
+            if (EDGE) {
+                // the scale of a token that a row does not see may be NaN
+                if (s[0][2 * n] == 0.f) y[0] = 0.f;
+                if (s[0][2 * n + 1] == 0.f) y[1] = 0.f;
+                if (s[1][2 * n] == 0.f) y[2] = 0.f;
+                if (s[1][2 * n + 1] == 0.f) y[3] = 0.f;
+            }
+            b[n][0] = pack_f16x2(y[0], y[1]);
+            b[n][1] = pack_f16x2(y[2], y[3]);
+            if (HL) {
+                const float2 c0 = f16x2_floats(b[n][0]), c1 = f16x2_floats(b[n][1]);
+                bl[n][0] = pack_f16x2(y[0] - c0.x, y[1] - c0.y);
+                bl[n][1] = pack_f16x2(y[2] - c1.x, y[3] - c1.y);
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t w0 = h ? vw0.w[j] >> 8 : vw0.w[j], w1 = h ? vw1.w[j] >> 8 : vw1.w[j];
+            const uint32_t a0 = w0 & 0x000f000fu, a1 = w0 & 0x00f000f0u, a2 = w1 & 0x000f000fu, a3 = w1 & 0x00f000f0u;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                mma_f16(st.o[2 * j + h][n], a0, a1, a2, a3, b[n][0], b[n][1]);
+                if (HL) mma_f16(st.o[2 * j + h][n], a0, a1, a2, a3, bl[n][0], bl[n][1]);
+            }
+        }
+    }
+}
+
+// A warp's state into its slot of the merge buffer: O [RT][D + 4], and (m, l) per row.
+template <int KIND, int D, int NT>
+__device__ inline void put_state(State<D, NT>& st, float* o, float2* ml, int lane) {
+    constexpr int DP = D + 4, NG = D / 32;
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        float l = st.l[n];
+        l += __shfl_xor_sync(kFull, l, 1);
+        l += __shfl_xor_sync(kFull, l, 2);
+        if (t == 0) ml[8 * n + g] = make_float2(st.m[n], l);
+        float* r0 = o + (8 * n + 2 * t) * DP;
+        float* r1 = r0 + DP;
+        if (KIND == MKV_INT4) {
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                const float z0 = __shfl_sync(kFull, st.lowest[n][0], j * 4 + t), z1 = __shfl_sync(kFull, st.lowest[n][1], j * 4 + t);
+                const float *x = st.o[2 * j][n], *y = st.o[2 * j + 1][n];
+                constexpr float e = 16777216.f, f = 1048576.f;   // 2^24, 2^20
+                *reinterpret_cast<float4*>(r0 + 32 * j + 4 * g) =
+                    make_float4(fmaf(x[0], e, z0), fmaf(x[2], f, z0), fmaf(y[0], e, z0), fmaf(y[2], f, z0));
+                *reinterpret_cast<float4*>(r1 + 32 * j + 4 * g) =
+                    make_float4(fmaf(x[1], e, z1), fmaf(x[3], f, z1), fmaf(y[1], e, z1), fmaf(y[3], f, z1));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                r0[16 * i + g] = st.o[i][n][0]; r1[16 * i + g] = st.o[i][n][1];
+                r0[16 * i + g + 8] = st.o[i][n][2]; r1[16 * i + g + 8] = st.o[i][n][3];
+            }
+        }
+    }
+}
+
+template <int KIND, int D, int NT, bool Q32, bool HL>
+__global__ void __launch_bounds__(kThreads, KIND == MKV_INT4 && NT == 1 ? 2 : 1)
+paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendArgs a, long long layer_rows) {
+    using C = Cfg<KIND, D, NT>;
+    constexpr int RT = C::RT, DP = C::DP;
+    extern __shared__ uint8_t raw_smem[];
+    __shared__ __align__(8) unsigned long long bars[kW * C::kStages];
+    __shared__ Unit s_unit;
+    __shared__ long long s_scan[kW + 1];
+    __shared__ int s_last;
+    uint8_t* const smem = raw_smem + ((1024u - (ptx::smem_u32(raw_smem) & 1023u)) & 1023u);
+    float* const merge = reinterpret_cast<float*>(smem + C::kRing);
+    float2* const mls = reinterpret_cast<float2*>(smem + C::kRing + C::kMerge);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (tid == 0) {
+        for (int i = 0; i < kW * C::kStages; ++i) ptx::mbar_init(ptx::smem_u32(&bars[i]), 1);
+        ptx::fence_barrier_init();
+    }
+    // ---- the list of blocks: its length, and where this CTA's range begins
+    const int per = (a.b.batch + kThreads - 1) / kThreads, s0 = tid * per, s1 = min(a.b.batch, s0 + per);
+    long long mine = 0;
+    for (int s = s0; s < s1; ++s) {
+        const PagedSpan sp = paged_span(a.c, a.b, s);
+        if (sp.n > a.max_new) paged_fail(a.c, MKV_ERR_CAPACITY);
+        mine += blocks_per_head<RT>(a, sp) * a.c.kv_heads;
+    }
+    long long before = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(kFull, before, o);
+        if (lane >= o) before += x;
+    }
+    if (lane == 31) s_scan[warp] = before;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int w = 0; w < kW; ++w) {
+        if (w < warp) before += s_scan[w];
+        total += s_scan[w];
+    }
+    before -= mine;
+    if (total == 0) return;
+    // a block for every warp at least, and no more ranges in a unit than its end can join quickly
+    long long ranges = max(1ll, min((long long)gridDim.x, total / kW));
+    if (a.b.batch * a.c.kv_heads < (int)gridDim.x / kMaxParts + 1) ranges = min(ranges, (long long)kMaxParts * a.b.batch * a.c.kv_heads);
+    const int n = (int)ranges;
+    if (blockIdx.x >= n) return;
+    const long long t0 = total * blockIdx.x / n, t1 = total * (blockIdx.x + 1) / n;
+    if (before <= t0 && t0 < before + mine) {
+        Unit u;
+        long long base = before;
+        for (int s = s0; s < s1; ++s) {
+            const PagedSpan sp = paged_span(a.c, a.b, s);
+            const long long head = blocks_per_head<RT>(a, sp), all = head * a.c.kv_heads;
+            if (t0 < base + all) {
+                u.s = s; u.tok0 = sp.tok0; u.n = sp.n; u.len = sp.len;
+                u.h = (int)((t0 - base) / head);
+                u.base = base + u.h * head;
+                u.rt = 0;
+                unit_rows<RT>(a, u);
+                while (u.end() <= t0) { u.base = u.end(); ++u.rt; unit_rows<RT>(a, u); }
+                break;
+            }
+            base += all;
+        }
+        s_unit = u;
+    }
+    __syncthreads();
+
+    // ---- this warp's fetches: unit f, blocks f_lo + warp, + kW, ... of its part [f_lo, f_hi) in the range
+    const uint32_t ring = ptx::smem_u32(smem) + warp * C::kStages * C::kStage;
+    const uint32_t bar0 = ptx::smem_u32(&bars[warp * C::kStages]);
+    Unit f = s_unit;
+    Unit u = f;
+    bool more = true;
+    int f_i = warp, f_n, f_first, page_of = 0, f_stage = 0, in_flight = 0;
+    auto enter = [&]() {
+        const long long lo = max(f.base, t0), hi = min(f.end(), t1);
+        f_first = f.blk0 + (int)(lo - f.base);
+        f_n = f.nblk == 0 ? 0 : (int)(hi - lo);
+        f_i = warp;
+    };
+    // one more block on its way, if there is one
+    auto fetch = [&]() {
+        while (more && f_i >= f_n) {
+            if (f.end() >= t1 || !next_unit<RT>(a, f)) more = false;
+            else enter();
+        }
+        if (!more) return;
+        const int k = (f_i - warp) / kW;
+        if ((k & 31) == 0) {   // pages of the next 32 blocks, one per lane
+            const int i = f_i + lane * kW;
+            page_of = i < f_n ? paged_page(a.c, a.b, f.s, (f_first + i) << 4) : 0;
+        }
+        const int page = __shfl_sync(kFull, page_of, k & 31);
+        const int row = ((f_first + f_i) << 4) & ((1 << a.c.page_shift) - 1);
+        if (lane == 0) {
+            const uint32_t dst = ring + f_stage * C::kStage, bar = bar0 + f_stage * 8;
+            ptx::mbar_arrive_expect_tx(bar, C::kStage);
+            if (KIND == MKV_INT4) {
+                ptx::bulk_g2s(dst, a.c.pages + (size_t)page * a.c.page_bytes + (size_t)f.h * a.c.head_bytes + (size_t)(row >> 4) * C::kStage,
+                              C::kStage, bar);
+            } else {
+                const int kv = a.c.kv_heads << a.c.page_shift;
+                const int y = (int)(layer_rows + (long long)page * 2 * kv) + (f.h << a.c.page_shift) + row;
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c) {
+                    tma_2d(dst + c * 2048, &map, 64 * c, y, bar);
+                    tma_2d(dst + 16 * D * 2 + c * 2048, &map, 64 * c, y + kv, bar);
+                }
+            }
+        }
+        f_stage = f_stage + 1 == C::kStages ? 0 : f_stage + 1;
+        ++in_flight;
+        f_i += kW;
+    };
+    enter();
+#pragma unroll 1
+    for (int i = 0; i < C::kStages; ++i) fetch();
+
+    // ---- units of the range
+    State<D, NT> st;
+    int stage = 0, parity = 0;
+    bool ok = true;
+    for (;;) {
+        const long long lo = max(u.base, t0), hi = min(u.end(), t1);
+        const int first = u.blk0 + (int)(lo - u.base), cnt = u.nblk == 0 ? 0 : (int)(hi - lo);
+        int pos[NT];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            pos[i] = u.len - u.n + (u.row0 + min((lane >> 2) + 8 * i, u.rows - 1)) / a.c.group;
+            st.m[i] = -FLT_MAX; st.l[i] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                st.lowest[i][e] = 0.f;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) st.o[k][i][e] = 0.f;
+            }
+        }
+        if (warp < cnt) {
+            typename std::conditional<KIND == MKV_INT4, QInt4<D, NT, Q32>, QBf16<D, NT>>::type q;
+            load_q(a, u, q, lane);
+            for (int i = warp; i < cnt; i += kW) {
+                if (ok && !ptx::mbar_wait_bounded(bar0 + stage * 8, parity, kWaitNs)) {
+                    ok = false;
+                    if (lane == 0) paged_fail(a.c, MKV_ERR_TIMEOUT);
+                }
+                ok = __all_sync(kFull, ok);
+                if (!ok) continue;   // the result is lost; what is on its way is waited for at the end
+                const int tok = (first + i) << 4;
+                const bool edge = tok + 15 > u.plo || (a.window > 0 && tok <= u.phi - a.window);
+                const uint32_t at = ring + stage * C::kStage;
+                if constexpr (KIND == MKV_INT4) {
+                    if (edge) block_int4<D, NT, Q32, HL, true>(st, q, a, u, pos, at, tok, lane);
+                    else block_int4<D, NT, Q32, HL, false>(st, q, a, u, pos, at, tok, lane);
+                } else {
+                    if (edge) block_bf16<D, NT, true>(st, q, a, u, pos, at, tok, lane);
+                    else block_bf16<D, NT, false>(st, q, a, u, pos, at, tok, lane);
+                }
+                __syncwarp();
+                --in_flight;
+                if (++stage == C::kStages) { stage = 0; parity ^= 1; }
+                fetch();
+            }
+        }
+        put_state<KIND, D, NT>(st, merge + warp * RT * DP, mls + warp * RT, lane);
+        __syncthreads();
+        // ---- the warps' states become one
+        const bool whole = lo == u.base && hi == u.end();
+        const Part part = part_at<RT, D>(a, 2 * blockIdx.x + (t0 < u.base ? 1 : 0));
+        for (int i = tid; i < RT * (D / 4); i += kThreads) {
+            const int row = i / (D / 4), c = (i - row * (D / 4)) * 4;
+            float m = -FLT_MAX, l = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kW; ++w) m = fmaxf(m, mls[w * RT + row].x);
+#pragma unroll
+            for (int w = 0; w < kW; ++w) {
+                const float2 x = mls[w * RT + row];
+                const float f2 = ex2(x.x - m);
+                const float4 y = *reinterpret_cast<const float4*>(merge + (w * RT + row) * DP + c);
+                l = fmaf(x.y, f2, l);
+                o.x = fmaf(y.x, f2, o.x); o.y = fmaf(y.y, f2, o.y); o.z = fmaf(y.z, f2, o.z); o.w = fmaf(y.w, f2, o.w);
+            }
+            if (whole) {
+                if (row < u.rows) store_row<D>(a, u, row, c, o, m, l);
+            } else {
+                *reinterpret_cast<float4*>(part.o + row * D + c) = o;
+                if (c == 0) { part.m[row] = m; part.l[row] = l; }
+            }
+        }
+        if (!whole) {
+            // the ranges that this unit spans: first and last
+            auto range_of = [&](long long t) {
+                int r = (int)(t * n / total);
+                while (total * (r + 1) / n <= t) ++r;
+                while (total * r / n > t) --r;
+                return r;
+            };
+            const int c0 = range_of(u.base), c1 = range_of(u.end() - 1);
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                int* ticket = reinterpret_cast<int*>(a.scratch) + c0;
+                s_last = atomicAdd(ticket, 1) == c1 - c0;
+                if (s_last) *ticket = 0;   // for the next launch
+                __threadfence();
+            }
+            __syncthreads();
+            if (s_last) {
+                for (int i = tid; i < u.rows * (D / 4); i += kThreads) {
+                    const int row = i / (D / 4), c = (i - row * (D / 4)) * 4;
+                    float m = -FLT_MAX, l = 0.f;
+                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                    const int first_slot = 2 * c0 + (total * c0 / n < u.base ? 1 : 0);
+                    for (int r = c0; r <= c1; ++r) {
+                        const Part p = part_at<RT, D>(a, r == c0 ? first_slot : 2 * r);
+                        const float pm = __ldcg(p.m + row), pl = __ldcg(p.l + row);
+                        const float4 y = __ldcg(reinterpret_cast<const float4*>(p.o + row * D + c));
+                        const float mn = fmaxf(m, pm), f1 = ex2(m - mn), f2 = ex2(pm - mn);
+                        l = fmaf(pl, f2, l * f1);
+                        o.x = fmaf(y.x, f2, o.x * f1); o.y = fmaf(y.y, f2, o.y * f1);
+                        o.z = fmaf(y.z, f2, o.z * f1); o.w = fmaf(y.w, f2, o.w * f1);
+                        m = mn;
+                    }
+                    store_row<D>(a, u, row, c, o, m, l);
+                }
+            }
+        }
+        if (u.end() >= t1 || !next_unit<RT>(a, u)) break;
+        __syncthreads();   // the merge buffer is free again
+    }
+    // copies still on their way after a wait that ran out
+    while (in_flight > 0) {
+        ptx::mbar_wait_bounded(bar0 + stage * 8, parity, kWaitNs);
+        if (++stage == C::kStages) { stage = 0; parity ^= 1; }
+        --in_flight;
+    }
+}
+
+template <int KIND, int D, int NT, bool Q32, bool HL>
+cudaError_t decode_t(const PagedAttendArgs& a, const CUtensorMap& map, long long layer_rows, int sm_count, cudaStream_t st) {
+    using C = Cfg<KIND, D, NT>;
+    auto* fn = paged_decode_kernel<KIND, D, NT, Q32, HL>;
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+    if (e != cudaSuccess) return e;
+    const int grid = min(sm_count * (KIND == MKV_INT4 && NT == 1 ? 2 : 1), kPagedTickets);
+    fn<<<grid, kThreads, C::kSmem, st>>>(map, a, layer_rows);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t paged_decode_scratch() { return kPagedTickets * 4 + (size_t)2 * kPagedTickets * 16 * (128 + 2) * 4; }
+
+bool make_paged_map(void* map, const void* pages, long long rows, int head_dim) {
+    using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess || !fn)
+        return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)head_dim, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)head_dim * 2};
+    const cuuint32_t box[2] = {64, 16}, step[2] = {1, 1};
+    return ((Encode)fn)((CUtensorMap*)map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pages), dims, strides, box, step,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t launch_paged_decode(const PagedAttendArgs& a, int D, const void* map, long long layer_rows, int sm_count, cudaStream_t st) {
+    const CUtensorMap& m = *(const CUtensorMap*)map;
+    const bool one = (long long)a.c.group * a.max_new <= 8;
+#define MKV_GO(KIND, NT, Q32, HL)                                                                  \
+    return D == 128 ? decode_t<KIND, 128, NT, Q32, HL>(a, m, layer_rows, sm_count, st)             \
+                    : decode_t<KIND, 64, NT, Q32, HL>(a, m, layer_rows, sm_count, st)
+    if (a.c.kv_dtype == MKV_BF16) {
+        if (one) { MKV_GO(MKV_BF16, 1, false, false); }
+        MKV_GO(MKV_BF16, 2, false, false);
+    }
+    if (a.c.io_f32) { MKV_GO(MKV_INT4, 1, true, true); }
+    if (a.c.out_f32) {
+        if (one) { MKV_GO(MKV_INT4, 1, false, true); }
+        MKV_GO(MKV_INT4, 2, false, true);
+    }
+    if (one) { MKV_GO(MKV_INT4, 1, false, false); }
+    MKV_GO(MKV_INT4, 2, false, false);
+#undef MKV_GO
+}
+
+}  // namespace mkv

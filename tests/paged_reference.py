@@ -70,6 +70,14 @@ def cache_values(pages, kind, layer, d, page_size):
     return p[:, 0].double(), p[:, 1].double()
 
 
+def cache_sizes(pages, kind, layer, d, page_size):
+    """What the kernels' products are made of, in size: |row|, and for 4 bits scale * code + |lowest|, whose two
+    terms are multiplied and summed apart (a small value may be the difference of two large ones)."""
+    if kind != INT4:
+        return tuple(x.abs() for x in cache_values(pages, kind, layer, d, page_size))
+    return tuple(int4_values(c, s, low.abs()) for c, s, low in int4_parts(pages[layer], d, page_size))
+
+
 def rows_of(values, table_row, length, page_size):
     """[kv_heads, length, d] of one sequence."""
     n = -(-length // page_size)
@@ -77,10 +85,11 @@ def rows_of(values, table_row, length, page_size):
     return values[at].transpose(0, 1).flatten(1, 2)[:, :length]
 
 
-def attend(q, K, V, first_pos, window=0, scale=0.0):
+def attend(q, K, V, first_pos, window=0, scale=0.0, sizes=None):
     """q [n, q_heads, d], K, V [kv_heads, length, d], fp64.  The query i stands at first_pos + i.
     Returns out, lse, and per row and channel what a bound on the error needs: the mean of |v| under the
-    weights, and the largest sum of |q k| * scale."""
+    weights, and the largest sum of |q k| * scale, with `sizes` (cache_sizes) in the place of |k| and |v|."""
+    KS, VS = (K.abs(), V.abs()) if sizes is None else sizes
     n, hq, d = q.shape
     hk, L = K.shape[:2]
     scale = scale or 1 / math.sqrt(d)
@@ -98,14 +107,16 @@ def attend(q, K, V, first_pos, window=0, scale=0.0):
         lse[i] = torch.logsumexp(s, -1).reshape(hq)
         p = torch.softmax(s, -1)
         out[i] = torch.einsum("hgl,hld->hgd", p, v).reshape(hq, d)
-        mean_abs[i] = torch.einsum("hgl,hld->hgd", p, v.abs()).reshape(hq, d)
-        s_abs[i] = (torch.einsum("hgd,hld->hgl", qi.abs(), k.abs()) * scale).amax(-1).reshape(hq)
+        mean_abs[i] = torch.einsum("hgl,hld->hgd", p, VS[:, begin:end]).reshape(hq, d)
+        s_abs[i] = (torch.einsum("hgd,hld->hgl", qi.abs(), KS[:, begin:end]) * scale).amax(-1).reshape(hq)
     return out, lse, mean_abs, s_abs
 
 
 # Errors of the kernels relative to exact arithmetic, each a bound:
 #   out = sum p v / sum p.  A relative error e_p of every p and e_v of every v changes out by at most
-#   (2 e_p + e_v) * mean|v|; p = exp(s) turns an absolute error of s into a relative one.
+#   (2 e_p + e_v) * mean|v|; p = exp(s) turns an absolute error of s into a relative one.  Over 4-bit pages
+#   v = scale * code + lowest enters as two products whose weights are rounded apart: |v| is
+#   scale * code + |lowest| there, and |k| in the sums of s likewise.
 #   s is a sum of d products accumulated in 32 bits (d roundings of at most 2^-23 of sum|q k| each, the
 #   matrix units may cut off instead of rounding), times constants (3 roundings), minus a maximum and
 #   into ex2.approx (2^-22): d_s = s_abs * (d + 8) * 2^-23, e_p0 = 2 d_s + 2^-21.

@@ -147,12 +147,13 @@ class Case:
 
     def compare(self, q, out, ls, e_p, e_k=0.0, e_v=0.0, window=0, scale=0.0):
         K, V = R.cache_values(self.pages, self.kind, self.layer, self.d, self.page)
+        KS, VS = R.cache_sizes(self.pages, self.kind, self.layer, self.d, self.page)
         for b, (a, e) in enumerate(zip(self.starts_h, self.starts_h[1:])):
             if e == a:
                 continue
             L = self.lens_h[b]
-            k, v = (R.rows_of(x, self.table_h[b].cuda(), L, self.page) for x in (K, V))
-            ref, lse, mean_abs, s_abs = R.attend(q[a:e].double(), k, v, L - (e - a), window, scale)
+            k, v, ks, vs = (R.rows_of(x, self.table_h[b].cuda(), L, self.page) for x in (K, V, KS, VS))
+            ref, lse, mean_abs, s_abs = R.attend(q[a:e].double(), k, v, L - (e - a), window, scale, (ks, vs))
             bound = R.out_bound(ref, mean_abs, s_abs, self.d, L, HALF[self.out], e_p, e_k, e_v)
             err = (out[a:e].double() - ref).abs()
             assert torch.isfinite(out[a:e]).all(), f"sequence {b}"
@@ -457,10 +458,11 @@ def test_what_is_not_seen_has_no_influence(kind, new):
     c.ctx.status_sync()
     assert torch.isnan(out[bad]).all() and torch.isfinite(out[~bad]).all()
     K, V = R.cache_values(c.pages, kind, 0, 128, 16)
+    KS, VS = R.cache_sizes(c.pages, kind, 0, 128, 16)
     rd = roundings(kind, c.out, 2 * new)
     for b in range(2):
-        k64, v64 = (R.rows_of(x, c.table[b], L, 16) for x in (K, V))
-        ref, rl, ma, sa = R.attend(q[b * new:(b + 1) * new].double(), k64, v64, L - new, window)
+        k64, v64, ks, vs = (R.rows_of(x, c.table[b], L, 16) for x in (K, V, KS, VS))
+        ref, rl, ma, sa = R.attend(q[b * new:(b + 1) * new].double(), k64, v64, L - new, window, sizes=(ks, vs))
         good = ~bad[b * new:(b + 1) * new].cuda()
         bound = R.out_bound(ref, ma, sa, 128, L, HALF[c.out], **rd)
         assert ((out[b * new:(b + 1) * new].double() - ref).abs() <= bound)[good].all()
