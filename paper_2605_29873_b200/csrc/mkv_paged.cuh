@@ -30,6 +30,7 @@ namespace mkv {
 constexpr int kPagedBlock = 16;     // tokens of a 4-bit block; also the granule of the attention kernels
 constexpr int kPagedMaxGroup = 32;  // q_heads / kv_heads
 constexpr int kPagedTickets = 1024;  // most CTAs of a launch that joins parts of units
+constexpr int kPagedTileCtas = 160;  // most CTAs of a launch of the kernel for many rows
 constexpr float kPagedNegInf = -INFINITY;
 
 struct PagedDev {
@@ -121,8 +122,12 @@ cudaError_t launch_paged_append(const PagedAppendArgs& a, int head_dim, cudaStre
 cudaError_t launch_paged_read(const PagedReadArgs& a, int head_dim, cudaStream_t st);
 cudaError_t launch_paged_simt(const PagedAttendArgs& a, int head_dim, cudaStream_t st);
 size_t paged_decode_scratch();   // workspace of launch_paged_decode, zero before its first launch
-bool make_paged_map(void* map, const void* pages, long long rows, int head_dim);   // bf16 pages as one list of rows
+bool make_paged_map(void* map, const void* pages, long long rows, int head_dim, int box_rows);   // bf16 pages as one list of rows
 cudaError_t launch_paged_decode(const PagedAttendArgs& a, int head_dim, const void* map, long long layer_rows, int sm_count,
                                 cudaStream_t st);
+
+size_t paged_tile_scratch();
+cudaError_t launch_paged_tile(const PagedAttendArgs& a, int head_dim, const void* map, long long layer_rows, int sm_count,
+                              cudaStream_t st);
 
 }  // namespace mkv

@@ -15,7 +15,7 @@ struct mkv_paged {
     int rot_dim, interleaved;
     int64_t launches;
     int sm_count;
-    alignas(64) CUtensorMap map;   // bf16: all pages as rows of head_dim
+    alignas(64) CUtensorMap map16, map_page;   // bf16: all pages as rows of head_dim, in boxes of 16 rows and of a page's
 };
 
 namespace {
@@ -26,7 +26,7 @@ PagedWs paged_ws() {
     w.status = 0;
     w.inv_freq = 256;
     w.scratch = 512;
-    w.total = (w.scratch + paged_decode_scratch() + 255) / 256 * 256;
+    w.total = (w.scratch + std::max(paged_decode_scratch(), paged_tile_scratch()) + 255) / 256 * 256;
     return w;
 }
 
@@ -128,8 +128,10 @@ mkv_status mkv_paged_create(int layers, int q_heads, int kv_heads, int head_dim,
     c->kv_dtype = kv_dtype; c->io_dtype = io_dtype; c->out_dtype = out_dtype; c->device = device;
     c->pages = (uint8_t*)pages; c->ws = (uint8_t*)workspace;
     c->rot_dim = 0; c->interleaved = 0; c->launches = 0;
+    const long long all_rows = (long long)layers * n_pages * 2 * kv_heads * page_size;
     if (cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
-        (kv_dtype == MKV_BF16 && !make_paged_map(&c->map, pages, (long long)layers * n_pages * 2 * kv_heads * page_size, head_dim))) {
+        (kv_dtype == MKV_BF16 && (!make_paged_map(&c->map16, pages, all_rows, head_dim, 16) ||
+                                  !make_paged_map(&c->map_page, pages, all_rows, head_dim, std::min(page_size, 128))))) {
         delete c;
         return MKV_ERR_CUDA;
     }
@@ -200,9 +202,11 @@ mkv_status mkv_paged_attend(mkv_paged* c, int layer, const void* q, int64_t q_st
     a.scale_log2 = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)c->head_dim)));
     a.scratch = c->ws + paged_ws().scratch;
     const long long rows_per_layer = (long long)c->n_pages * 2 * c->kv_heads * c->page_size;
-    const cudaError_t e = c->kv_dtype != MKV_F32 && (long long)a.c.group * a.max_new <= 64
-                              ? launch_paged_decode(a, c->head_dim, &c->map, layer * rows_per_layer, c->sm_count, (cudaStream_t)stream)
-                              : launch_paged_simt(a, c->head_dim, (cudaStream_t)stream);
+    const cudaStream_t st = (cudaStream_t)stream;
+    const cudaError_t e = c->kv_dtype == MKV_F32 ? launch_paged_simt(a, c->head_dim, st)
+                          : (long long)a.c.group * a.max_new <= 64
+                              ? launch_paged_decode(a, c->head_dim, &c->map16, layer * rows_per_layer, c->sm_count, st)
+                              : launch_paged_tile(a, c->head_dim, &c->map_page, layer * rows_per_layer, c->sm_count, st);
     if (e != cudaSuccess) return MKV_ERR_CUDA;
     c->launches += 1;
     return MKV_OK;

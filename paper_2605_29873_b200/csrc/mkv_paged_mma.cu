@@ -36,7 +36,7 @@
 #include <climits>
 #include <type_traits>
 
-#include "mkv_paged.cuh"
+#include "mkv_paged_units.cuh"
 #include "mkv_ptx.cuh"
 
 namespace mkv {
@@ -96,61 +96,6 @@ __device__ inline void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
         ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
-
-// One (sequence, KV head, row tile), and the part of the block list that is its own.
-struct Unit {
-    long long base;   // of its first block in the list
-    int s, h, rt;
-    int tok0, n, len;
-    int row0, rows;   // rows [row0, row0 + rows) of the n * group of its sequence and head
-    int plo, phi;     // positions of the first and the last row's token
-    int blk0, nblk;   // blocks to read; a unit without any counts as one in the list
-    __device__ int count() const { return max(nblk, 1); }
-    __device__ long long end() const { return base + count(); }
-};
-
-template <int RT>
-__device__ inline void unit_rows(const PagedAttendArgs& a, Unit& u) {
-    const int G = a.c.group, R = u.n * G;
-    u.row0 = u.rt * RT;
-    u.rows = min(RT, R - u.row0);
-    u.plo = u.len - u.n + u.row0 / G;
-    u.phi = u.len - u.n + (u.row0 + u.rows - 1) / G;
-    const int begin = a.window > 0 ? max(0, u.plo - a.window + 1) : 0;
-    u.blk0 = begin >> 4;
-    u.nblk = u.phi >= begin ? (u.phi >> 4) - u.blk0 + 1 : 0;
-}
-template <int RT> __device__ inline int row_tiles(const PagedAttendArgs& a, int n) { return (n * a.c.group + RT - 1) / RT; }
-
-// Blocks of one head of sequence s in the list.
-template <int RT>
-__device__ inline long long blocks_per_head(const PagedAttendArgs& a, const PagedSpan& sp) {
-    Unit u;
-    u.n = sp.n; u.len = sp.len;
-    long long t = 0;
-    const int rts = row_tiles<RT>(a, sp.n);
-    for (u.rt = 0; u.rt < rts; ++u.rt) { unit_rows<RT>(a, u); t += u.count(); }
-    return t;
-}
-
-// Moves u to the next unit that has rows; false behind the last.
-template <int RT>
-__device__ inline bool next_unit(const PagedAttendArgs& a, Unit& u) {
-    u.base = u.end();
-    if (++u.rt >= row_tiles<RT>(a, u.n)) {
-        u.rt = 0;
-        if (++u.h >= a.c.kv_heads) {
-            u.h = 0;
-            do {
-                if (++u.s >= a.b.batch) return false;
-                const PagedSpan sp = paged_span(a.c, a.b, u.s);
-                u.tok0 = sp.tok0; u.n = sp.n; u.len = sp.len;
-            } while (u.n == 0);
-        }
-    }
-    unit_rows<RT>(a, u);
-    return true;
 }
 
 struct Part { float *o, *m, *l; };
@@ -636,7 +581,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
     extern __shared__ uint8_t raw_smem[];
     __shared__ __align__(8) unsigned long long bars[kW * C::kStages];
     __shared__ Unit s_unit;
-    __shared__ long long s_scan[kW + 1];
+    __shared__ long long s_scan[kW];
     __shared__ int s_last;
     uint8_t* const smem = raw_smem + ((1024u - (ptx::smem_u32(raw_smem) & 1023u)) & 1023u);
     float* const merge = reinterpret_cast<float*>(smem + C::kRing);
@@ -647,56 +592,14 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
         for (int i = 0; i < kW * C::kStages; ++i) ptx::mbar_init(ptx::smem_u32(&bars[i]), 1);
         ptx::fence_barrier_init();
     }
-    // ---- the list of blocks: its length, and where this CTA's range begins
-    const int per = (a.b.batch + kThreads - 1) / kThreads, s0 = tid * per, s1 = min(a.b.batch, s0 + per);
-    long long mine = 0;
-    for (int s = s0; s < s1; ++s) {
-        const PagedSpan sp = paged_span(a.c, a.b, s);
-        if (sp.n > a.max_new) paged_fail(a.c, MKV_ERR_CAPACITY);
-        mine += blocks_per_head<RT>(a, sp) * a.c.kv_heads;
-    }
-    long long before = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long x = __shfl_up_sync(kFull, before, o);
-        if (lane >= o) before += x;
-    }
-    if (lane == 31) s_scan[warp] = before;
-    __syncthreads();
-    long long total = 0;
-#pragma unroll
-    for (int w = 0; w < kW; ++w) {
-        if (w < warp) before += s_scan[w];
-        total += s_scan[w];
-    }
-    before -= mine;
-    if (total == 0) return;
     // a block for every warp at least, and no more ranges in a unit than its end can join quickly
-    long long ranges = max(1ll, min((long long)gridDim.x, total / kW));
-    if (a.b.batch * a.c.kv_heads < (int)gridDim.x / kMaxParts + 1) ranges = min(ranges, (long long)kMaxParts * a.b.batch * a.c.kv_heads);
-    const int n = (int)ranges;
-    if (blockIdx.x >= n) return;
-    const long long t0 = total * blockIdx.x / n, t1 = total * (blockIdx.x + 1) / n;
-    if (before <= t0 && t0 < before + mine) {
-        Unit u;
-        long long base = before;
-        for (int s = s0; s < s1; ++s) {
-            const PagedSpan sp = paged_span(a.c, a.b, s);
-            const long long head = blocks_per_head<RT>(a, sp), all = head * a.c.kv_heads;
-            if (t0 < base + all) {
-                u.s = s; u.tok0 = sp.tok0; u.n = sp.n; u.len = sp.len;
-                u.h = (int)((t0 - base) / head);
-                u.base = base + u.h * head;
-                u.rt = 0;
-                unit_rows<RT>(a, u);
-                while (u.end() <= t0) { u.base = u.end(); ++u.rt; unit_rows<RT>(a, u); }
-                break;
-            }
-            base += all;
-        }
-        s_unit = u;
-    }
-    __syncthreads();
+    Range rg;
+    if (!find_range<RT, 16, kThreads>(a, rg, &s_unit, s_scan, [&](long long total) {
+            const long long units = (long long)a.b.batch * a.c.kv_heads;
+            return min(total / kW, units * kMaxParts);
+        }))
+        return;
+    const long long t0 = rg.t0, t1 = rg.t1;
 
     // ---- this warp's fetches: unit f, blocks f_lo + warp, + kW, ... of its part [f_lo, f_hi) in the range
     const uint32_t ring = ptx::smem_u32(smem) + warp * C::kStages * C::kStage;
@@ -714,7 +617,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
     // one more block on its way, if there is one
     auto fetch = [&]() {
         while (more && f_i >= f_n) {
-            if (f.end() >= t1 || !next_unit<RT>(a, f)) more = false;
+            if (f.end() >= t1 || !next_unit<RT, 16>(a, f)) more = false;
             else enter();
         }
         if (!more) return;
@@ -822,13 +725,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
         }
         if (!whole) {
             // the ranges that this unit spans: first and last
-            auto range_of = [&](long long t) {
-                int r = (int)(t * n / total);
-                while (total * (r + 1) / n <= t) ++r;
-                while (total * r / n > t) --r;
-                return r;
-            };
-            const int c0 = range_of(u.base), c1 = range_of(u.end() - 1);
+            const int c0 = rg.of(u.base), c1 = rg.of(u.end() - 1);
             __threadfence();
             __syncthreads();
             if (tid == 0) {
@@ -843,7 +740,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
                     const int row = i / (D / 4), c = (i - row * (D / 4)) * 4;
                     float m = -FLT_MAX, l = 0.f;
                     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                    const int first_slot = 2 * c0 + (total * c0 / n < u.base ? 1 : 0);
+                    const int first_slot = 2 * c0 + (rg.begin_of(c0) < u.base ? 1 : 0);
                     for (int r = c0; r <= c1; ++r) {
                         const Part p = part_at<RT, D>(a, r == c0 ? first_slot : 2 * r);
                         const float pm = __ldcg(p.m + row), pl = __ldcg(p.l + row);
@@ -858,7 +755,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
                 }
             }
         }
-        if (u.end() >= t1 || !next_unit<RT>(a, u)) break;
+        if (u.end() >= t1 || !next_unit<RT, 16>(a, u)) break;
         __syncthreads();   // the merge buffer is free again
     }
     // copies still on their way after a wait that ran out
@@ -884,7 +781,7 @@ cudaError_t decode_t(const PagedAttendArgs& a, const CUtensorMap& map, long long
 
 size_t paged_decode_scratch() { return kPagedTickets * 4 + (size_t)2 * kPagedTickets * 16 * (128 + 2) * 4; }
 
-bool make_paged_map(void* map, const void* pages, long long rows, int head_dim) {
+bool make_paged_map(void* map, const void* pages, long long rows, int head_dim, int box_rows) {
     using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -894,7 +791,7 @@ bool make_paged_map(void* map, const void* pages, long long rows, int head_dim) 
         found != cudaDriverEntryPointSuccess || !fn)
         return false;
     const cuuint64_t dims[2] = {(cuuint64_t)head_dim, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)head_dim * 2};
-    const cuuint32_t box[2] = {64, 16}, step[2] = {1, 1};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, step[2] = {1, 1};
     return ((Encode)fn)((CUtensorMap*)map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pages), dims, strides, box, step,
                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

@@ -1,0 +1,818 @@
+// Attention over the paged cache for many rows (pieces of prompts): tensor-core bound, tcgen05.
+//
+// A unit is one (sequence, KV head, 256 rows of new token x query head), worked through in tiles of 128
+// cached tokens; the list of all units' tiles is cut into one contiguous range per CTA (see
+// mkv_paged_units.cuh), parts of a unit are joined by the CTA that delivers the last one, in order.
+//
+// A CTA is a pipeline over its tiles.  Its 256 rows are two halves of 128, one row per thread of a
+// softmax warpgroup:
+//   MMA thread   S_h = Q_h K^T (shared memory x shared memory -> tensor memory, 128 x 128 fp32), then
+//                O_h += P_h V (tensor memory x shared memory), for the halves in turn: while one half's
+//                products run, the other half's softmax does.
+//   softmax      reads its row of S, p = 2^(s - m), writes P over S as 16-bit.  m is a reference that
+//                moves only when a logit exceeds it by 2^8; O is rescaled then, by the row's own thread.
+//   producer     bf16 pages: bulk tensor copies, 128-byte swizzle.  4-bit pages: a warpgroup turns codes into
+//                fp16 rows (value / 2^f, f by the tile's largest, so that fp16 holds any cache), the
+//                next tile's words already in registers.
+// Tensor memory: S0 S1 O0 O1, 128 columns each.  Shared memory (head_dim 128): Q 64 KB, two stages of K and V
+// 128 KB.
+// The second product's weights are one bf16 (2^-9 rounding, as the values they multiply have), over 4-bit pages
+// one fp16.  Sums, references and O are fp32; the sum of p is taken before the rounding.
+#include <cuda.h>
+#include <cuda_fp16.h>
+#include <cfloat>
+#include <climits>
+
+#include "mkv_paged_units.cuh"
+#include "mkv_ptx.cuh"
+
+namespace mkv {
+namespace {
+
+constexpr int kRows = 256, kTile = 128;
+constexpr int kSoft = 256;                  // softmax threads
+constexpr unsigned long long kWaitNs = 2000000000ull;
+constexpr unsigned kFull = 0xffffffffu;
+// Tokens with non-finite values that only some rows of a unit see.  A unit has at most 2 x 255 of them (the
+// diagonal and the window's edge), and the producers are at most three units ahead.
+constexpr int kOddMax = 2048;
+
+template <int KIND> __host__ __device__ constexpr int threads_of() { return kSoft + (KIND == MKV_INT4 ? 128 + 32 : 64); }
+
+template <int D>
+struct TileCfg {
+    static constexpr int kHalf = 128 * D * 2;         // 128 rows of 16-bit channels: Q half, K tile, V tile
+    static constexpr int kSmem = 1024 + 6 * kHalf;    // Q0 Q1, K x 2, V x 2
+};
+
+// ---- tcgen05 and friends
+__device__ inline void tmem_alloc(uint32_t dst, int cols) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ inline void tmem_free(uint32_t addr, int cols) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
+}
+__device__ inline void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ inline void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ inline void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ inline void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+__device__ inline void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+#define MKV_R8(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
+#define MKV_I8(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
+// 32 columns of this thread's lane
+__device__ inline void tmem_ld32(uint32_t addr, uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : MKV_R8(v, 0), MKV_R8(v, 8), MKV_R8(v, 16), MKV_R8(v, 24) : "r"(addr));
+}
+__device__ inline void tmem_st32(uint32_t addr, const uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+        ::MKV_I8(v, 0), MKV_I8(v, 8), MKV_I8(v, 16), MKV_I8(v, 24), "r"(addr) : "memory");
+}
+__device__ inline void tmem_st16(uint32_t addr, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+        ::MKV_I8(v, 0), MKV_I8(v, 8), "r"(addr) : "memory");
+}
+__device__ inline void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ inline void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Shared-memory operand with 128-byte rows of 64 channels, 128-byte swizzle: groups of 8 rows are 1024 bytes.
+// `lead`: bytes to the next 64 channels where the channels are the operand's outer dimension (V).
+__device__ inline uint64_t smem_desc(uint32_t addr, uint32_t lead) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// fp32 accumulator, A and B both bf16 (1) or fp16 (0), M = 128, N columns; `b_outer`: B's outer dimension is contiguous
+__host__ __device__ constexpr uint32_t mma_desc(int type, int n, bool b_outer) {
+    return 1u << 4 | (uint32_t)type << 7 | (uint32_t)type << 10 | (uint32_t)b_outer << 16 | (uint32_t)(n >> 3) << 17 | (128u >> 4) << 24;
+}
+
+__device__ inline float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ inline uint32_t pack_f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ inline void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ inline void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ inline void sts64(uint32_t addr, uint32_t a, uint32_t b) {
+    asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
+// 16-byte chunk c of row r of a tile of 128 rows, 64 channels (8 chunks) next to one another
+__device__ inline uint32_t chunk_at(uint32_t tile, int r, int c) { return tile + (c >> 3) * (128 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
+
+struct Shared {
+    unsigned long long q_full[2], s_full[2], p_full[2], o_full[2];
+    unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2];
+    uint32_t tmem;
+    int dead;                       // a wait ran out: everybody leaves
+    int last;
+    int n_odd;
+    int2 odd[kOddMax];              // (tile of this CTA, position), a ring
+    float k_mul[2], v_exp[2];       // 4 bits: what the stage's K and V were divided by (a factor, a log2)
+    float red[8];
+    long long scan[16];
+    Unit unit;
+};
+
+// Waits that end: false once any of the CTA's waits ran out.
+__device__ inline bool wait_or_leave(const PagedAttendArgs& a, Shared& sh, uint32_t bar, uint32_t parity) {
+    if (*(volatile int*)&sh.dead) return false;
+    if (ptx::mbar_wait_bounded(bar, parity, kWaitNs)) return true;
+    *(volatile int*)&sh.dead = 1;
+    paged_fail(a.c, MKV_ERR_TIMEOUT);
+    return false;
+}
+
+// Whether anybody of the softmax threads gives up; a barrier for all of them.
+__device__ inline bool any_leaves(bool leave) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r) : "r"((uint32_t)leave) : "memory");
+    return r != 0;
+}
+__device__ inline void soft_barrier() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
+
+struct TilePart { float *o, *m, *l; };
+template <int D>
+__device__ inline TilePart tile_part(const PagedAttendArgs& a, int slot) {
+    float* p = reinterpret_cast<float*>(a.scratch + kPagedTickets * 4) + (size_t)slot * kRows * (D + 2);
+    return {p, p + kRows * D, p + kRows * D + kRows};
+}
+
+// position of row r (of the unit's) and where its output goes
+struct RowPlace { int pos; size_t at; };
+__device__ inline RowPlace row_place(const PagedAttendArgs& a, const Unit& u, int r) {
+    const int x = u.row0 + min(r, u.rows - 1), j = x / a.c.group;
+    return {u.len - u.n + j, (size_t)(u.tok0 + j) * a.c.q_heads + u.h * a.c.group + (x - j * a.c.group)};
+}
+
+// 32 channels of a row, o / l
+template <int D>
+__device__ inline void store32(const PagedAttendArgs& a, size_t at, int c, const float (&o)[32], float inv) {
+    if (a.c.out_f32) {
+        float4* p = reinterpret_cast<float4*>((float*)a.out + at * D + c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = make_float4(o[4 * i] * inv, o[4 * i + 1] * inv, o[4 * i + 2] * inv, o[4 * i + 3] * inv);
+    } else {
+        uint4* p = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + at * D + c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            p[i] = make_uint4(ptx::pack_bf16x2(o[8 * i] * inv, o[8 * i + 1] * inv), ptx::pack_bf16x2(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
+                              ptx::pack_bf16x2(o[8 * i + 4] * inv, o[8 * i + 5] * inv), ptx::pack_bf16x2(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
+    }
+}
+
+// Cached V value of channel c at position p (only for tokens with non-finite values)
+template <int KIND, int D>
+__device__ inline float v_value(const PagedAttendArgs& a, const Unit& u, int p, int c) {
+    const uint8_t* head = a.c.pages + (size_t)paged_page(a.c, a.b, u.s, p) * a.c.page_bytes + (size_t)u.h * a.c.head_bytes;
+    const int row = p & ((1 << a.c.page_shift) - 1);
+    if (KIND == MKV_BF16) return __bfloat162float(((const __nv_bfloat16*)(head + a.c.kv_bytes))[(size_t)row * D + c]);
+    constexpr int NG = D / 32;
+    const uint8_t* par = head + (size_t)(row >> 4) * paged_block_bytes(D) + 16 * D + 64 * NG;
+    return paged_bf16(*(const uint16_t*)(par + (((row & 15) >> 1) * NG + (c >> 5)) * 4 + (row & 1) * 2));   // its NaN scale
+}
+
+// ---- softmax threads: this thread's row of half w
+template <int KIND, int D, bool IO32>
+__device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const Range& rg, uint32_t smem) {
+    using C = TileCfg<D>;
+    const int tid = threadIdx.x, w = tid >> 7, row = tid & 127, warp4 = (tid >> 5) & 3;
+    const uint32_t lanes = (uint32_t)(warp4 * 32) << 16;
+    const uint32_t sT = sh.tmem + lanes + w * 128, oT = sh.tmem + lanes + 256 + w * 128;
+    const uint32_t q_full = ptx::smem_u32(&sh.q_full[w]), s_full = ptx::smem_u32(&sh.s_full[w]), p_full = ptx::smem_u32(&sh.p_full[w]),
+                   o_full = ptx::smem_u32(&sh.o_full[w]);
+    const uint32_t q_smem = smem + w * C::kHalf, v_smem = smem + 4 * C::kHalf;
+    uint32_t s_par = 0, o_par = 0;
+    int tiles = 0;            // of this CTA so far: stage and parity of K and V
+    Unit u = sh.unit;
+    for (;;) {
+        const long long lo = max(u.base, rg.t0), hi = min(u.end(), rg.t1);
+        const int first = u.blk0 + (int)(lo - u.base), nt = u.nblk == 0 ? 0 : (int)(hi - lo);
+        const bool active = w == 0 || u.rows > 128;
+        const int r = w * 128 + row;
+        const RowPlace place = row_place(a, u, r);
+        const bool live = r < u.rows;
+        float m = -FLT_MAX, l = 0.f, back = a.scale_log2;
+        if (nt > 0 && active) {
+            // ---- Q: this thread's row
+            if (KIND == MKV_BF16) {
+                const uint4* src = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + (place.at / a.c.q_heads) * a.q_stride + (place.at % a.c.q_heads) * D);
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    const uint4 x = live ? src[c] : make_uint4(0, 0, 0, 0);
+                    sts128(chunk_at(q_smem, row, c), x.x, x.y, x.z, x.w);
+                }
+            } else {
+                // fp16, scaled by a power of two to [2^13, 2^14); channels of eight in the order 0 4 1 5 2 6 3 7, as
+                // the codes' nibbles come (K has the same order)
+                const size_t at = (place.at / a.c.q_heads) * a.q_stride + (place.at % a.c.q_heads) * D;
+                float big = 0.f;
+                auto load8 = [&](int c, float (&x)[8]) {
+                    if (IO32) {
+                        const float4 v0 = reinterpret_cast<const float4*>((const float*)a.q + at)[2 * c], v1 = reinterpret_cast<const float4*>((const float*)a.q + at)[2 * c + 1];
+                        x[0] = v0.x; x[1] = v0.y; x[2] = v0.z; x[3] = v0.w; x[4] = v1.x; x[5] = v1.y; x[6] = v1.z; x[7] = v1.w;
+                    } else {
+                        const uint4 v = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + at)[c];
+                        const uint32_t z[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { x[2 * e] = __uint_as_float(z[e] << 16); x[2 * e + 1] = __uint_as_float(z[e] & 0xffff0000u); }
+                    }
+                };
+#pragma unroll 4
+                for (int c = 0; c < D / 8; ++c) {
+                    float x[8];
+                    load8(c, x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(x[e]));
+                }
+                const int ex = min(max((int)(__float_as_uint(big) >> 23), 16), 254);
+                const float up = __uint_as_float((uint32_t)min(254, 127 + 13 + 127 - ex) << 23);
+                back = a.scale_log2 * (1.f / up);
+#pragma unroll 4
+                for (int c = 0; c < D / 8; ++c) {
+                    float x[8];
+                    load8(c, x);
+                    const float z = live ? up : 0.f;
+                    sts128(chunk_at(q_smem, row, c), live ? pack_f16x2(x[0] * z, x[4] * z) : 0u, live ? pack_f16x2(x[1] * z, x[5] * z) : 0u,
+                           live ? pack_f16x2(x[2] * z, x[6] * z) : 0u, live ? pack_f16x2(x[3] * z, x[7] * z) : 0u);
+                }
+            }
+            ptx::fence_proxy_async();
+            ptx::mbar_arrive(q_full);
+        }
+        bool ok = true;
+        if (active) {
+            for (int j = 0; j < nt; ++j) {
+                const int stage = (tiles + j) & 1;
+                const uint32_t par = ((tiles + j) >> 1) & 1;
+                const int t0 = (first + j) * kTile;
+                const bool edge = t0 + kTile - 1 > u.plo || (a.window > 0 && t0 <= u.phi - a.window);
+                if (edge && w == 0 && KIND == MKV_BF16) {
+                    // V rows that no row sees may hold anything: zero.  Of rows that some see, what is not finite is
+                    // taken out (it must not meet the others' zero weights) and added at the end.
+                    if (!(ok = __all_sync(kFull, wait_or_leave(a, sh, ptx::smem_u32(&sh.v_full[stage]), par)))) break;
+                    const int p = t0 + row, begin = a.window > 0 ? u.plo - a.window + 1 : 0;
+                    const bool none = p > u.phi || p < begin;
+                    const bool some = !none && (p > u.plo || (a.window > 0 && p <= u.phi - a.window));
+                    if (none || some) {
+                        bool odd = false;
+#pragma unroll 4
+                        for (int i = 0; i < D / 8; ++i) {
+                            const uint32_t at = chunk_at(v_smem + stage * C::kHalf, row, (i & 8) | ((i + row) & 7));
+                            if (none) { sts128(at, 0, 0, 0, 0); continue; }
+                            uint32_t x[4];
+                            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at));
+                            bool hit = false;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                if ((x[e] & 0x7f80u) == 0x7f80u) { x[e] &= 0xffff0000u; hit = true; }
+                                if ((x[e] & 0x7f800000u) == 0x7f800000u) { x[e] &= 0xffffu; hit = true; }
+                            }
+                            if (hit) sts128(at, x[0], x[1], x[2], x[3]);
+                            odd |= hit;
+                        }
+                        if (odd) {
+                            sh.odd[atomicAdd(&sh.n_odd, 1) % kOddMax] = make_int2(tiles + j, p);
+                        }
+                        ptx::fence_proxy_async();
+                    }
+                }
+                if (!(ok = __all_sync(kFull, wait_or_leave(a, sh, s_full, s_par)))) break;
+                s_par ^= 1;
+                fence_after();
+                float mul = back, f = 0.f;
+                if (KIND == MKV_INT4) {
+                    if (!(ok = __all_sync(kFull, wait_or_leave(a, sh, ptx::smem_u32(&sh.v_full[stage]), par)))) break;
+                    mul *= sh.k_mul[stage];
+                    f = sh.v_exp[stage];
+                }
+                const int top = place.pos - t0, bottom = a.window > 0 ? top - a.window : INT_MIN;   // bottom < column <= top
+                uint32_t v[32];
+                float mx = kPagedNegInf;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    tmem_ld32(sT + 32 * c, v);
+                    wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        float s = __uint_as_float(v[e]);
+                        if (edge && (32 * c + e > top || 32 * c + e <= bottom)) s = kPagedNegInf;
+                        mx = fmaxf(mx, s);
+                    }
+                }
+                mx = fmaf(mx, mul, f);
+                const bool move = mx > m + 8.f;
+                if (__any_sync(kFull, move)) {
+                    const float mn = move ? mx : m, sc = ex2(m - mn);
+                    m = mn;
+                    l *= sc;
+                    if (j > 0) {   // the products before are complete: this tile's S was issued behind them
+#pragma unroll 1
+                        for (int c = 0; c < D / 32; ++c) {
+                            tmem_ld32(oT + 32 * c, v);
+                            wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * sc);
+                            tmem_st32(oT + 32 * c, v);
+                        }
+                        wait_st();
+                    }
+                }
+                const float ref = f - m;
+                float sum = 0.f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    tmem_ld32(sT + 32 * c, v);
+                    wait_ld();
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        float s0 = __uint_as_float(v[e]), s1 = __uint_as_float(v[e + 1]);
+                        if (edge) {
+                            if (32 * c + e > top || 32 * c + e <= bottom) s0 = kPagedNegInf;
+                            if (32 * c + e + 1 > top || 32 * c + e + 1 <= bottom) s1 = kPagedNegInf;
+                        }
+                        const float p0 = ex2(fmaf(s0, mul, ref)), p1 = ex2(fmaf(s1, mul, ref));
+                        sum += p0 + p1;
+                        pk[e >> 1] = KIND == MKV_BF16 ? ptx::pack_bf16x2(p0, p1) : pack_f16x2(p0, p1);
+                    }
+                    tmem_st16(sT + 16 * c, pk);
+                }
+                l += KIND == MKV_INT4 ? sum * ex2(-f) : sum;
+                wait_st();
+                fence_before();
+                ptx::mbar_arrive(p_full);
+            }
+        }
+        if (active && nt > 0 && ok) {
+            ok = wait_or_leave(a, sh, o_full, o_par);
+            o_par ^= 1;
+            fence_after();
+        }
+        if (any_leaves(!ok)) return;   // and the list of odd tokens is complete
+        // ---- the row's result, or its part
+        const bool whole = lo == u.base && hi == u.end();
+        const TilePart part = tile_part<D>(a, 2 * blockIdx.x + (rg.t0 < u.base ? 1 : 0));
+        if (active) {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const int n_odd = *(volatile int*)&sh.n_odd;
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                float o[32];
+                if (nt > 0) {
+                    uint32_t v[32];
+                    tmem_ld32(oT + 32 * c, v);
+                    wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(v[e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0.f;
+                }
+                for (int i = max(0, n_odd - kOddMax); i < n_odd; ++i) {
+                    const int2 x2 = sh.odd[i % kOddMax];
+                    const int p = x2.y;
+                    if (x2.x < tiles || x2.x >= tiles + nt || p > place.pos || (a.window > 0 && p <= place.pos - a.window)) continue;
+#pragma unroll 1
+                    for (int e = 0; e < 32; ++e) {
+                        const float x = v_value<KIND, D>(a, u, p, 32 * c + e);
+                        if (!isfinite(x)) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (k == e) o[k] += x;
+                        }
+                    }
+                }
+                if (!live) continue;
+                if (whole) {
+                    store32<D>(a, place.at, 32 * c, o, inv);
+                } else {
+                    float4* p = reinterpret_cast<float4*>(part.o + (size_t)r * D + 32 * c);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) p[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                }
+            }
+            fence_before();
+            if (live && whole && a.lse) a.lse[place.at] = l == 0.f ? kPagedNegInf : (m + log2f(l)) * 0.69314718055994531f;
+            if (live && !whole) { part.m[r] = m; part.l[r] = l; }
+        }
+        tiles += nt;
+        if (!whole) {
+            const int c0 = rg.of(u.base), c1 = rg.of(u.end() - 1);
+            __threadfence();
+            soft_barrier();
+            if (tid == 0) {
+                int* ticket = reinterpret_cast<int*>(a.scratch) + c0;
+                sh.last = atomicAdd(ticket, 1) == c1 - c0;
+                if (sh.last) *ticket = 0;   // for the next launch
+                __threadfence();
+            }
+            soft_barrier();
+            if (sh.last && live) {
+                const int slot0 = 2 * c0 + (rg.begin_of(c0) < u.base ? 1 : 0);
+                float mm = -FLT_MAX, ll = 0.f;
+                for (int x = c0; x <= c1; ++x) mm = fmaxf(mm, __ldcg(tile_part<D>(a, x == c0 ? slot0 : 2 * x).m + r));
+                for (int x = c0; x <= c1; ++x) {
+                    const TilePart p = tile_part<D>(a, x == c0 ? slot0 : 2 * x);
+                    ll = fmaf(__ldcg(p.l + r), ex2(__ldcg(p.m + r) - mm), ll);
+                }
+                const float inv = ll == 0.f ? 0.f : 1.f / ll;
+#pragma unroll 1
+                for (int c = 0; c < D / 32; ++c) {
+                    float o[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0.f;
+                    for (int x = c0; x <= c1; ++x) {
+                        const TilePart p = tile_part<D>(a, x == c0 ? slot0 : 2 * x);
+                        const float sc = ex2(__ldcg(p.m + r) - mm);
+                        const float4* y = reinterpret_cast<const float4*>(p.o + (size_t)r * D + 32 * c);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 z = __ldcg(y + i);
+                            o[4 * i] = fmaf(z.x, sc, o[4 * i]); o[4 * i + 1] = fmaf(z.y, sc, o[4 * i + 1]);
+                            o[4 * i + 2] = fmaf(z.z, sc, o[4 * i + 2]); o[4 * i + 3] = fmaf(z.w, sc, o[4 * i + 3]);
+                        }
+                    }
+                    store32<D>(a, place.at, 32 * c, o, inv);
+                }
+                if (a.lse) a.lse[place.at] = ll == 0.f ? kPagedNegInf : (mm + log2f(ll)) * 0.69314718055994531f;
+            }
+        }
+        if (u.end() >= rg.t1 || !next_unit<kRows, kTile>(a, u)) return;
+        soft_barrier();   // sh.last has been read
+    }
+}
+
+// ---- the MMA thread
+template <int KIND, int D>
+__device__ inline void mma_role(const PagedAttendArgs& a, Shared& sh, const Range& rg, uint32_t smem) {
+    using C = TileCfg<D>;
+    constexpr int kType = KIND == MKV_BF16 ? 1 : 0;
+    constexpr uint32_t qk = mma_desc(kType, kTile, false), pv = mma_desc(kType, D, true);
+    auto bar = [](unsigned long long& b) { return ptx::smem_u32(&b); };
+    uint32_t q_par = 0, q1_par = 0, p_par[2] = {0, 0};
+    int tiles = 0;
+    Unit u = sh.unit;
+    auto qk_product = [&](int w, int stage) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            const uint32_t off = (k >> 2) * (128 * 128) + (k & 3) * 32;
+            mma_ss(sh.tmem + w * 128, smem_desc(smem + w * C::kHalf + off, 16), smem_desc(smem + (2 + stage) * C::kHalf + off, 16), qk, k > 0);
+        }
+    };
+    auto pv_product = [&](int w, int stage, bool add) {
+#pragma unroll
+        for (int k = 0; k < kTile / 16; ++k)
+            mma_ts(sh.tmem + 256 + w * 128, sh.tmem + w * 128 + 8 * k, smem_desc(smem + (4 + stage) * C::kHalf + k * 2048, 128 * 128), pv, add || k > 0);
+    };
+    for (;;) {
+        const long long lo = max(u.base, rg.t0), hi = min(u.end(), rg.t1);
+        const int nt = u.nblk == 0 ? 0 : (int)(hi - lo);
+        const int halves = u.rows > 128 ? 2 : 1;
+        if (nt > 0) {
+            if (!wait_or_leave(a, sh, bar(sh.q_full[0]), q_par)) return;
+            q_par ^= 1;
+            if (halves == 2) {
+                if (!wait_or_leave(a, sh, bar(sh.q_full[1]), q1_par)) return;
+                q1_par ^= 1;
+            }
+            if (!wait_or_leave(a, sh, bar(sh.k_full[tiles & 1]), (tiles >> 1) & 1)) return;
+            fence_after();
+            for (int w = 0; w < halves; ++w) {
+                qk_product(w, tiles & 1);
+                mma_commit(bar(sh.s_full[w]));
+            }
+            mma_commit(bar(sh.k_empty[tiles & 1]));
+        }
+        for (int j = 0; j < nt; ++j) {
+            const int t = tiles + j, stage = t & 1, next = (t + 1) & 1;
+            const bool more = j + 1 < nt;
+            if (!wait_or_leave(a, sh, bar(sh.v_full[stage]), (t >> 1) & 1)) return;
+            if (more && !wait_or_leave(a, sh, bar(sh.k_full[next]), ((t + 1) >> 1) & 1)) return;
+            for (int w = 0; w < halves; ++w) {
+                if (!wait_or_leave(a, sh, bar(sh.p_full[w]), p_par[w])) return;
+                p_par[w] ^= 1;
+                fence_after();
+                pv_product(w, stage, j > 0);
+                if (w == halves - 1) mma_commit(bar(sh.v_empty[stage]));
+                if (more) {
+                    qk_product(w, next);
+                    mma_commit(bar(sh.s_full[w]));
+                } else {
+                    mma_commit(bar(sh.o_full[w]));
+                }
+            }
+            if (more) mma_commit(bar(sh.k_empty[next]));
+        }
+        tiles += nt;
+        if (u.end() >= rg.t1 || !next_unit<kRows, kTile>(a, u)) return;
+    }
+}
+
+// ---- bf16 pages: the thread that issues the copies
+template <int D>
+__device__ inline void copy_role(const PagedAttendArgs& a, Shared& sh, const Range& rg, uint32_t smem, const CUtensorMap* map,
+                                 long long layer_rows) {
+    using C = TileCfg<D>;
+    const int box = min(1 << a.c.page_shift, kTile);
+    const int kv = a.c.kv_heads << a.c.page_shift;
+    int tiles = 0;
+    Unit u = sh.unit;
+    bool ok = true;
+    for (; ok;) {
+        const long long lo = max(u.base, rg.t0), hi = min(u.end(), rg.t1);
+        const int first = u.blk0 + (int)(lo - u.base), nt = u.nblk == 0 ? 0 : (int)(hi - lo);
+        for (int j = 0; j < nt; ++j, ++tiles) {
+            const int stage = tiles & 1;
+            const uint32_t par = ((tiles >> 1) & 1) ^ 1;
+            const int t0 = (first + j) * kTile, n = min(kTile, (u.phi - t0) / box * box + box);   // rows of boxes that hold seen tokens
+            const uint32_t kf = ptx::smem_u32(&sh.k_full[stage]), vf = ptx::smem_u32(&sh.v_full[stage]);
+#pragma unroll 1
+            for (int which = 0; which < 2; ++which) {
+                const uint32_t full = which ? vf : kf, empty = ptx::smem_u32(which ? &sh.v_empty[stage] : &sh.k_empty[stage]);
+                if (tiles >= 2 && !(ok = wait_or_leave(a, sh, empty, par))) break;
+                ptx::mbar_arrive_expect_tx(full, (uint32_t)(n * D * 2));
+                const uint32_t dst = smem + (2 + 2 * which + stage) * C::kHalf;
+                for (int x = 0; x < n; x += box) {
+                    const int page = paged_page(a.c, a.b, u.s, t0 + x), row = (t0 + x) & ((1 << a.c.page_shift) - 1);
+                    const int y = (int)(layer_rows + (long long)page * 2 * kv) + which * kv + (u.h << a.c.page_shift) + row;
+#pragma unroll
+                    for (int c = 0; c < D / 64; ++c) tma_2d(dst + c * (128 * 128) + x * 128, map, 64 * c, y, full);
+                }
+            }
+            if (!ok) break;
+        }
+        if (!ok || u.end() >= rg.t1 || !next_unit<kRows, kTile>(a, u)) break;
+    }
+    // the CTA must not end with copies on their way: they are waited for by the products, except after a wait that ran out
+    if (*(volatile int*)&sh.dead)
+        for (int k = max(0, tiles - 2); k <= tiles; ++k) {
+            ptx::mbar_wait_bounded(ptx::smem_u32(&sh.k_full[k & 1]), (k >> 1) & 1, kWaitNs / 8);
+            ptx::mbar_wait_bounded(ptx::smem_u32(&sh.v_full[k & 1]), (k >> 1) & 1, kWaitNs / 8);
+        }
+}
+
+// ---- 4-bit pages: a warpgroup turns them into fp16 rows
+template <int D>
+struct RawTile {
+    static constexpr int NG = D / 32;
+    uint4 k[D / 32], v[D / 32];   // a token's K row; half of a token pair's V rows
+    uint32_t ks[NG], kl[NG / 2], vs[NG], vl[NG];
+};
+
+template <int D>
+__device__ inline void load_raw(const PagedAttendArgs& a, const Unit& u, int t0, int id, RawTile<D>& x) {
+    constexpr int NG = D / 32;
+    // K: token t0 + id.  V: pair of tokens t0 + 2 (id / 2), its lower or upper half of the words
+    const int p = t0 + id;
+#pragma unroll
+    for (int i = 0; i < NG; ++i) { x.k[i] = x.v[i] = make_uint4(0, 0, 0, 0); x.ks[i] = x.vs[i] = x.vl[i] = 0; }
+#pragma unroll
+    for (int i = 0; i < NG / 2; ++i) x.kl[i] = 0;
+    if ((p & ~15) > u.phi) return;
+    const uint8_t* head = a.c.pages + (size_t)paged_page(a.c, a.b, u.s, p & ~15) * a.c.page_bytes + (size_t)u.h * a.c.head_bytes;
+    const int row = p & ((1 << a.c.page_shift) - 1), r = row & 15;
+    const uint8_t* blk = head + (size_t)(row >> 4) * paged_block_bytes(D);
+    const uint4* kp = reinterpret_cast<const uint4*>(blk + r * (D / 2));
+    const uint4* vp = reinterpret_cast<const uint4*>(blk + 8 * D + (r >> 1) * D + (r & 1) * (D / 2));
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) { x.k[i] = __ldg(kp + i); x.v[i] = __ldg(vp + i); }
+    const uint32_t* par = reinterpret_cast<const uint32_t*>(blk + 16 * D);
+#pragma unroll
+    for (int j = 0; j < NG; ++j) {
+        x.ks[j] = __ldg(par + (r >> 1) * NG + j);
+        x.vs[j] = __ldg(par + 16 * NG + (r >> 1) * NG + j);
+        x.vl[j] = __ldg(par + 24 * NG + (r >> 1) * NG + j);
+    }
+#pragma unroll
+    for (int j = 0; j < NG / 2; ++j) x.kl[j] = __ldg(par + 8 * NG + r * (NG / 2) + j);
+}
+
+__device__ inline __half2 codes_low(uint32_t w) {    // nibbles 0 and 4 as numbers
+    const uint32_t x = (w & 0x000f000fu) | 0x64006400u;   // 1024 + n
+    return __hsub2(*(const __half2*)&x, __half2half2(__ushort_as_half(0x6400)));
+}
+__device__ inline __half2 codes_high(uint32_t w) {   // nibbles 1 and 5
+    const uint32_t x = (w & 0x00f000f0u) | 0x64006400u;   // 1024 + 16 n
+    return __hfma2(*(const __half2*)&x, __half2half2(__ushort_as_half(0x2c00)), __half2half2(__ushort_as_half(0xd400)));   // / 16 - 64
+}
+__device__ inline uint32_t as_u32(__half2 h) { return *(const uint32_t*)&h; }
+
+// largest |value| a group can have
+__device__ inline float group_top(float s, float l) {
+    const float t = fmaxf(fabsf(l), fabsf(fmaf(15.f, s, l)));
+    return t == t ? t : 0.f;
+}
+// f of the tile: values / 2^f are below 2^10, in the middle of what fp16 holds; kept where 2^-f and 2^f are normal
+__device__ inline float tile_exponent(Shared& sh, int id, float top) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
+    asm volatile("barrier.cta.sync 2, 128;" ::: "memory");
+    if ((id & 31) == 0) sh.red[id >> 5] = top;
+    asm volatile("barrier.cta.sync 2, 128;" ::: "memory");
+    top = fmaxf(fmaxf(sh.red[0], sh.red[1]), fmaxf(sh.red[2], sh.red[3]));
+    return (float)(min(max((int)(__float_as_uint(top) >> 23) - 126, -100), 104) - 10);
+}
+
+template <int D>
+__device__ inline void dequant_role(const PagedAttendArgs& a, Shared& sh, const Range& rg, uint32_t smem, int id) {
+    using C = TileCfg<D>;
+    constexpr int NG = D / 32;
+    int tiles = 0;
+    Unit u = sh.unit;
+    RawTile<D> x;
+    // the first tile's words; every later tile's are fetched while the one before is being written
+    auto part_of = [&](const Unit& y, int& first, int& nt) {
+        const long long lo = max(y.base, rg.t0), hi = min(y.end(), rg.t1);
+        first = y.blk0 + (int)(lo - y.base);
+        nt = y.nblk == 0 ? 0 : (int)(hi - lo);
+    };
+    int first, nt;
+    part_of(u, first, nt);
+    bool fresh = true;
+    for (;;) {
+        for (int j = 0; j < nt; ++j, ++tiles) {
+            const int stage = tiles & 1;
+            const uint32_t par = ((tiles >> 1) & 1) ^ 1;
+            const int t0 = (first + j) * kTile;
+            if (fresh) { load_raw<D>(a, u, t0, id, x); fresh = false; }
+            const int begin = a.window > 0 ? max(0, u.plo - a.window + 1) : 0;
+            const int p = t0 + id;
+            const bool seen = p <= u.phi && p >= begin, other = (p ^ 1) <= u.phi && (p ^ 1) >= begin;
+            // ---- K
+            float ktop = 0.f, s[NG], l[NG];
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const uint32_t ks = x.ks[g], kl = x.kl[g >> 1];
+                s[g] = __uint_as_float(id & 1 ? ks & 0xffff0000u : ks << 16);
+                l[g] = __uint_as_float(g & 1 ? kl & 0xffff0000u : kl << 16);
+                if (!seen) s[g] = l[g] = 0.f;
+                ktop = fmaxf(ktop, group_top(s[g], l[g]));
+            }
+            const float kf = tile_exponent(sh, id, ktop);
+            const float kdown = __uint_as_float((uint32_t)(127 - (int)kf) << 23);
+            if (tiles >= 2) wait_or_leave(a, sh, ptx::smem_u32(&sh.k_empty[stage]), par);   // goes on even then: its threads stay together
+            if (id == 0) sh.k_mul[stage] = __uint_as_float((uint32_t)(127 + (int)kf) << 23);
+            const uint32_t ktile = smem + (2 + stage) * C::kHalf;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                // 16 bytes = words (t, j): for D = 128 t = i, j = 0..3; for D = 64 t = 2 i + e / 2, j = e & 1
+                const uint32_t w4[4] = {x.k[i].x, x.k[i].y, x.k[i].z, x.k[i].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int t = NG == 4 ? i : 2 * i + (e >> 1), g = e & (NG - 1);
+                    const __half2 s2 = __float2half2_rn(s[g] * kdown), l2 = __float2half2_rn(l[g] * kdown);
+                    const uint32_t w = w4[e];
+                    sts128(chunk_at(ktile, id, 4 * g + t), as_u32(__hfma2(codes_low(w), s2, l2)), as_u32(__hfma2(codes_high(w), s2, l2)),
+                           as_u32(__hfma2(codes_low(w >> 8), s2, l2)), as_u32(__hfma2(codes_high(w >> 8), s2, l2)));
+                }
+            }
+            ptx::fence_proxy_async();
+            ptx::mbar_arrive(ptx::smem_u32(&sh.k_full[stage]));
+            // ---- V: tokens id & ~1 and its neighbour, words of g 0..3 or 4..7
+            const bool even_seen = id & 1 ? other : seen, odd_seen = id & 1 ? seen : other;
+            float vtop = 0.f, s0[NG], l0[NG], s1[NG], l1[NG];
+            bool odd0 = false, odd1 = false;
+            const int r0 = id & ~1, g0 = (id & 1) * 4;
+            auto some = [&](int r) { return t0 + r > u.plo || (a.window > 0 && t0 + r <= u.phi - a.window); };
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                s0[g] = __uint_as_float(x.vs[g] << 16); s1[g] = __uint_as_float(x.vs[g] & 0xffff0000u);
+                l0[g] = __uint_as_float(x.vl[g] << 16); l1[g] = __uint_as_float(x.vl[g] & 0xffff0000u);
+                if (!even_seen) s0[g] = l0[g] = 0.f;
+                if (!odd_seen) s1[g] = l1[g] = 0.f;
+                // a group of NaN that only some rows see: out of the product (it would meet the others' zero weights), added at the end
+                if (s0[g] != s0[g] && some(r0)) { odd0 = true; s0[g] = l0[g] = 0.f; }
+                if (s1[g] != s1[g] && some(r0 + 1)) { odd1 = true; s1[g] = l1[g] = 0.f; }
+                vtop = fmaxf(vtop, fmaxf(group_top(s0[g], l0[g]), group_top(s1[g], l1[g])));
+            }
+            const float vf = tile_exponent(sh, id, vtop);
+            const float vdown = __uint_as_float((uint32_t)(127 - (int)vf) << 23);
+            if (tiles >= 2) wait_or_leave(a, sh, ptx::smem_u32(&sh.v_empty[stage]), par);
+            if (id == 0) sh.v_exp[stage] = vf;
+            if ((id & 1) == 0 && (odd0 || odd1)) {
+                if (odd0) sh.odd[atomicAdd(&sh.n_odd, 1) % kOddMax] = make_int2(tiles, p);
+                if (odd1) sh.odd[atomicAdd(&sh.n_odd, 1) % kOddMax] = make_int2(tiles, p + 1);
+            }
+            const uint32_t vtile = smem + (4 + stage) * C::kHalf;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                // words (g, j): for D = 128 g = g0 + i, j = 0..3; for D = 64 g = g0 + 2 i + e / 2, j = e & 1
+                const uint32_t w4[4] = {x.v[i].x, x.v[i].y, x.v[i].z, x.v[i].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int g = g0 + (NG == 4 ? i : 2 * i + (e >> 1)), j = e & (NG - 1);
+                    const __half2 s2 = __floats2half2_rn(s0[j] * vdown, s1[j] * vdown), l2 = __floats2half2_rn(l0[j] * vdown, l1[j] * vdown);
+                    const uint32_t w = w4[e];
+                    // halves: even token, odd token; four channels
+                    const uint32_t c0 = as_u32(__hfma2(codes_low(w), s2, l2)), c1 = as_u32(__hfma2(codes_high(w), s2, l2));
+                    const uint32_t c2 = as_u32(__hfma2(codes_low(w >> 8), s2, l2)), c3 = as_u32(__hfma2(codes_high(w >> 8), s2, l2));
+                    const uint32_t off = (g & 1) * 8;
+                    sts64(chunk_at(vtile, r0, 4 * j + (g >> 1)) + off, __byte_perm(c0, c1, 0x5410), __byte_perm(c2, c3, 0x5410));
+                    sts64(chunk_at(vtile, r0 + 1, 4 * j + (g >> 1)) + off, __byte_perm(c0, c1, 0x7632), __byte_perm(c2, c3, 0x7632));
+                }
+            }
+            ptx::fence_proxy_async();
+            ptx::mbar_arrive(ptx::smem_u32(&sh.v_full[stage]));
+            if (j + 1 < nt) load_raw<D>(a, u, t0 + kTile, id, x);
+        }
+        if (u.end() >= rg.t1 || !next_unit<kRows, kTile>(a, u)) return;
+        part_of(u, first, nt);
+        fresh = true;
+    }
+}
+
+template <int KIND, int D, bool IO32>
+__global__ void __launch_bounds__(threads_of<KIND>(), 1)
+paged_tile_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendArgs a, long long layer_rows) {
+    using C = TileCfg<D>;
+    extern __shared__ uint8_t raw_smem[];
+    __shared__ Shared sh;
+    const uint32_t smem = (ptx::smem_u32(raw_smem) + 1023u) & ~1023u;
+    const int tid = threadIdx.x, warp = tid >> 5;
+    Range rg;
+    // a few tiles for a range, so that joining parts does not outweigh them
+    if (!find_range<kRows, kTile, threads_of<KIND>()>(a, rg, &sh.unit, sh.scan, [](long long total) { return (total + 1) / 2; })) return;
+    if (tid == 0) {
+        auto init = [](unsigned long long& b, int n) { ptx::mbar_init(ptx::smem_u32(&b), n); };
+        for (int i = 0; i < 2; ++i) {
+            init(sh.q_full[i], 128); init(sh.s_full[i], 1); init(sh.p_full[i], 128); init(sh.o_full[i], 1);
+            init(sh.k_full[i], KIND == MKV_INT4 ? 128 : 1); init(sh.v_full[i], KIND == MKV_INT4 ? 128 : 1);
+            init(sh.k_empty[i], 1); init(sh.v_empty[i], 1);
+        }
+        sh.dead = 0;
+        sh.n_odd = 0;
+        ptx::fence_barrier_init();
+    }
+    if (warp == 0) tmem_alloc(ptx::smem_u32(&sh.tmem), 512);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (tid < kSoft) {
+        softmax_role<KIND, D, IO32>(a, sh, rg, smem);
+    } else if (KIND == MKV_INT4) {
+        if (tid < kSoft + 128) dequant_role<D>(a, sh, rg, smem, tid - kSoft);
+        else if (tid == kSoft + 128) mma_role<KIND, D>(a, sh, rg, smem);
+    } else {
+        if (tid == kSoft) copy_role<D>(a, sh, rg, smem, &map, layer_rows);
+        else if (tid == kSoft + 32) mma_role<KIND, D>(a, sh, rg, smem);
+    }
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    if (warp == 0) tmem_free(sh.tmem, 512);
+}
+
+template <int KIND, int D, bool IO32>
+cudaError_t tile_t(const PagedAttendArgs& a, const CUtensorMap& map, long long layer_rows, int sm_count, cudaStream_t st) {
+    auto* fn = paged_tile_kernel<KIND, D, IO32>;
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, TileCfg<D>::kSmem);
+    if (e != cudaSuccess) return e;
+    fn<<<min(sm_count, kPagedTileCtas), threads_of<KIND>(), TileCfg<D>::kSmem, st>>>(map, a, layer_rows);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t paged_tile_scratch() { return kPagedTickets * 4 + (size_t)2 * kPagedTileCtas * kRows * (128 + 2) * 4; }
+
+cudaError_t launch_paged_tile(const PagedAttendArgs& a, int D, const void* map, long long layer_rows, int sm_count, cudaStream_t st) {
+    const CUtensorMap& m = *(const CUtensorMap*)map;
+    if (a.c.kv_dtype == MKV_BF16)
+        return D == 128 ? tile_t<MKV_BF16, 128, false>(a, m, layer_rows, sm_count, st) : tile_t<MKV_BF16, 64, false>(a, m, layer_rows, sm_count, st);
+    if (a.c.io_f32)
+        return D == 128 ? tile_t<MKV_INT4, 128, true>(a, m, layer_rows, sm_count, st) : tile_t<MKV_INT4, 64, true>(a, m, layer_rows, sm_count, st);
+    return D == 128 ? tile_t<MKV_INT4, 128, false>(a, m, layer_rows, sm_count, st) : tile_t<MKV_INT4, 64, false>(a, m, layer_rows, sm_count, st);
+}
+
+}  // namespace mkv

@@ -172,15 +172,16 @@ class Case:
 # (2^-17 of the value is left) over bf16 pages, as one fp16 (2^-11), or a sum of two where out is fp32,
 # over 4-bit pages, whose lowest values meet them as a sum of two bf16; as they are over fp32 pages.
 # From 65 rows (tokens x group) of a sequence and head on, a tile kernel takes over: weights one bf16
-# (2^-8) over bf16 pages; over 4-bit pages one fp16, and the rows themselves rounded to fp16 (2^-11).
-def roundings(kind, out, rows):
+# (2^-8) over bf16 pages; over 4-bit pages one fp16, and the rows themselves rounded to fp16 (2^-11), fp32
+# queries too (another 2^-11 of every product).
+def roundings(kind, out, rows, io=BF16):
     tiles = rows > 64
     if kind == F32:
         return dict(e_p=0.0)
     if kind == BF16:
         return dict(e_p=2.0 ** -8 if tiles else 2.0 ** -16)
     if tiles:
-        return dict(e_p=2.0 ** -11, e_k=2.0 ** -11, e_v=2.0 ** -11)
+        return dict(e_p=2.0 ** -11, e_k=2.0 ** (-10 if io == F32 else -11), e_v=2.0 ** -11)
     return dict(e_p=2.0 ** -11 if out == BF16 else 2.0 ** -15)
 
 
@@ -415,7 +416,7 @@ def test_attend_several_tokens(case):
     kind, io, out, d, hq, hk, page, lens, new, window = MANY[case]
     c = Case(kind, hq, hk, d, page, lens, new, io=io, out=out, seed=100 + case, pad_tokens=2)
     c.fill()
-    c.check_attend(window=window, **roundings(kind, c.out, hq // hk * max(new)))
+    c.check_attend(window=window, **roundings(kind, c.out, hq // hk * max(new), c.io))
 
 
 @pytest.mark.gpu
