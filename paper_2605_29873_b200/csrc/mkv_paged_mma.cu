@@ -37,14 +37,12 @@
 #include <type_traits>
 
 #include "mkv_paged_units.cuh"
-#include "mkv_ptx.cuh"
 
 namespace mkv {
 namespace {
 
 constexpr int kW = 8;                       // warps of a CTA
 constexpr int kThreads = kW * 32;
-constexpr unsigned long long kWaitNs = 2000000000ull;
 constexpr int kMaxParts = 64;               // ranges that may share one unit
 constexpr unsigned kFull = 0xffffffffu;
 
@@ -675,7 +673,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
             typename std::conditional<KIND == MKV_INT4, QInt4<D, NT, Q32>, QBf16<D, NT>>::type q;
             load_q(a, u, q, lane);
             for (int i = warp; i < cnt; i += kW) {
-                if (ok && !ptx::mbar_wait_bounded(bar0 + stage * 8, parity, kWaitNs)) {
+                if (ok && !paged_wait(bar0 + stage * 8, parity)) {
                     ok = false;
                     if (lane == 0) paged_fail(a.c, MKV_ERR_TIMEOUT);
                 }
@@ -760,7 +758,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
     }
     // copies still on their way after a wait that ran out
     while (in_flight > 0) {
-        ptx::mbar_wait_bounded(bar0 + stage * 8, parity, kWaitNs);
+        paged_wait(bar0 + stage * 8, parity);
         if (++stage == C::kStages) { stage = 0; parity ^= 1; }
         --in_flight;
     }

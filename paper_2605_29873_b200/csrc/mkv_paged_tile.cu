@@ -24,14 +24,12 @@
 #include <climits>
 
 #include "mkv_paged_units.cuh"
-#include "mkv_ptx.cuh"
 
 namespace mkv {
 namespace {
 
 constexpr int kRows = 256, kTile = 128;
 constexpr int kSoft = 256;                  // softmax threads
-constexpr unsigned long long kWaitNs = 2000000000ull;
 constexpr unsigned kFull = 0xffffffffu;
 // Tokens with non-finite values that only some rows of a unit see.  A unit has at most 2 x 255 of them (the
 // diagonal and the window's edge), and the producers are at most three units ahead.
@@ -42,7 +40,9 @@ template <int KIND> __host__ __device__ constexpr int threads_of() { return kSof
 template <int D>
 struct TileCfg {
     static constexpr int kHalf = 128 * D * 2;         // 128 rows of 16-bit channels: Q half, K tile, V tile
-    static constexpr int kSmem = 1024 + 6 * kHalf;    // Q0 Q1, K x 2, V x 2
+    // rows on their way out, 8 KB a warp: over Q, or behind everything where Q's rows are shorter than that
+    static constexpr int kOut = D == 128 ? 0 : 6 * kHalf;
+    static constexpr int kSmem = 1024 + 6 * kHalf + (D == 128 ? 0 : 65536);    // Q0 Q1, K x 2, V x 2
 };
 
 // ---- tcgen05 and friends
@@ -124,6 +124,11 @@ __device__ inline void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c,
 __device__ inline void sts64(uint32_t addr, uint32_t a, uint32_t b) {
     asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
 }
+__device__ inline uint4 lds128(uint32_t addr) {
+    uint4 x;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(addr));
+    return x;
+}
 // 16-byte chunk c of row r of a tile of 128 rows, 64 channels (8 chunks) next to one another
 __device__ inline uint32_t chunk_at(uint32_t tile, int r, int c) { return tile + (c >> 3) * (128 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
 
@@ -144,7 +149,7 @@ struct Shared {
 // Waits that end: false once any of the CTA's waits ran out.
 __device__ inline bool wait_or_leave(const PagedAttendArgs& a, Shared& sh, uint32_t bar, uint32_t parity) {
     if (*(volatile int*)&sh.dead) return false;
-    if (ptx::mbar_wait_bounded(bar, parity, kWaitNs)) return true;
+    if (paged_wait(bar, parity)) return true;
     *(volatile int*)&sh.dead = 1;
     paged_fail(a.c, MKV_ERR_TIMEOUT);
     return false;
@@ -161,7 +166,12 @@ __device__ inline bool any_leaves(bool leave) {
 }
 __device__ inline void soft_barrier() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
 
-struct TilePart { float *o, *m, *l; };
+// A part of a unit in the workspace: four channels of all 256 rows, the next four, ... (a warp's rows next to one
+// another), then m and l.
+struct TilePart {
+    float *o, *m, *l;
+    __device__ float4* at(int row, int c) const { return reinterpret_cast<float4*>(o) + (c >> 2) * kRows + row; }
+};
 template <int D>
 __device__ inline TilePart tile_part(const PagedAttendArgs& a, int slot) {
     float* p = reinterpret_cast<float*>(a.scratch + kPagedTickets * 4) + (size_t)slot * kRows * (D + 2);
@@ -169,25 +179,50 @@ __device__ inline TilePart tile_part(const PagedAttendArgs& a, int slot) {
 }
 
 // position of row r (of the unit's) and where its output goes
-struct RowPlace { int pos; size_t at; };
+struct RowPlace { int pos, tok, head; size_t at; };
 __device__ inline RowPlace row_place(const PagedAttendArgs& a, const Unit& u, int r) {
     const int x = u.row0 + min(r, u.rows - 1), j = x / a.c.group;
-    return {u.len - u.n + j, (size_t)(u.tok0 + j) * a.c.q_heads + u.h * a.c.group + (x - j * a.c.group)};
+    const int head = u.h * a.c.group + (x - j * a.c.group);
+    return {u.len - u.n + j, u.tok0 + j, head, (size_t)(u.tok0 + j) * a.c.q_heads + head};
 }
 
-// 32 channels of a row, o / l
+// The rows of a warp on their way out: every lane has its row's 16-byte chunks put() into the warp's 8 KB of shared
+// memory (that of its Q rows, free by then; chunk c of row r at c ^ (r & 15)), then 16 lanes write 256 bytes of
+// a row at a time.
+struct RowsOut {
+    uint32_t slice;
+    int lane;
+    __device__ void put(int c, uint32_t x, uint32_t y, uint32_t z, uint32_t w) const {
+        sts128(slice + lane * 256 + ((c ^ (lane & 15)) << 4), x, y, z, w);
+    }
+    // bytes: of a row that were put (<= 256).  `dst`: this lane's row, or nullptr
+    __device__ void flush(uint8_t* dst, int bytes) const {
+        __syncwarp();
+#pragma unroll 4
+        for (int i = 0; i < 32; i += 2) {
+            const int r = i + (lane >> 4), c = lane & 15;
+            uint8_t* p = reinterpret_cast<uint8_t*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(dst), r));
+            if (p && 16 * c < bytes) *reinterpret_cast<uint4*>(p + 16 * c) = lds128(slice + r * 256 + ((c ^ (r & 15)) << 4));
+        }
+        __syncwarp();
+    }
+};
+
+// 32 channels of every lane's row, o / l; a row is complete after the last.  `dst`: this lane's row, or nullptr
 template <int D>
-__device__ inline void store32(const PagedAttendArgs& a, size_t at, int c, const float (&o)[32], float inv) {
+__device__ inline void store32(const PagedAttendArgs& a, const RowsOut& out, uint8_t* dst, int c, const float (&o)[32], float inv) {
     if (a.c.out_f32) {
-        float4* p = reinterpret_cast<float4*>((float*)a.out + at * D + c);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = make_float4(o[4 * i] * inv, o[4 * i + 1] * inv, o[4 * i + 2] * inv, o[4 * i + 3] * inv);
+        for (int i = 0; i < 8; ++i)
+            out.put((c & 32) / 4 + i, __float_as_uint(o[4 * i] * inv), __float_as_uint(o[4 * i + 1] * inv), __float_as_uint(o[4 * i + 2] * inv),
+                    __float_as_uint(o[4 * i + 3] * inv));
+        if (c & 32) out.flush(dst ? dst + (c - 32) * 4 : nullptr, 256);
     } else {
-        uint4* p = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + at * D + c);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            p[i] = make_uint4(ptx::pack_bf16x2(o[8 * i] * inv, o[8 * i + 1] * inv), ptx::pack_bf16x2(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
-                              ptx::pack_bf16x2(o[8 * i + 4] * inv, o[8 * i + 5] * inv), ptx::pack_bf16x2(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
+            out.put(c / 8 + i, ptx::pack_bf16x2(o[8 * i] * inv, o[8 * i + 1] * inv), ptx::pack_bf16x2(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
+                    ptx::pack_bf16x2(o[8 * i + 4] * inv, o[8 * i + 5] * inv), ptx::pack_bf16x2(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
+        if (c == D - 32) out.flush(dst, D * 2);
     }
 }
 
@@ -202,15 +237,110 @@ __device__ inline float v_value(const PagedAttendArgs& a, const Unit& u, int p, 
     return paged_bf16(*(const uint16_t*)(par + (((row & 15) >> 1) * NG + (c >> 5)) * 4 + (row & 1) * 2));   // its NaN scale
 }
 
+__device__ inline float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+__device__ inline uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ inline float2 unpair(uint64_t x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ inline uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ inline uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+template <bool EDGE>
+__device__ inline void hide(uint32_t (&v)[32], int c, int top, int bottom) {
+    if (!EDGE) return;
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+        if (c + e > top || c + e <= bottom) v[e] = 0xff800000u;
+}
+__device__ inline void max32(const uint32_t (&v)[32], float (&mx)[4]) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 8)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(v[e + 2 * k]), __uint_as_float(v[e + 2 * k + 1]));
+}
+// Largest visible logit of the row (bottom < column <= top), 32 columns on their way while 32 are looked at.
+template <bool EDGE>
+__device__ inline float row_max(uint32_t sT, int top, int bottom) {
+    float mx[4] = {kPagedNegInf, kPagedNegInf, kPagedNegInf, kPagedNegInf};
+    uint32_t x[32], y[32];
+    tmem_ld32(sT, x);
+#pragma unroll 1
+    for (int c = 0; c < kTile; c += 64) {
+        wait_ld();
+        tmem_ld32(sT + c + 32, y);
+        hide<EDGE>(x, c, top, bottom);
+        max32(x, mx);
+        wait_ld();
+        if (c + 64 < kTile) tmem_ld32(sT + c + 64, x);
+        hide<EDGE>(y, c + 32, top, bottom);
+        max32(y, mx);
+    }
+    return fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+}
+template <int KIND>
+__device__ inline void weights32(const uint32_t (&v)[32], uint32_t pT, uint64_t mul, uint64_t ref, uint64_t (&sum)[2]) {
+    uint32_t pk[16];
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+        const float2 x = unpair(fma2(pair(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), mul, ref));
+        const float p0 = ex2(x.x), p1 = ex2(x.y);
+        sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pair(p0, p1));
+        pk[e >> 1] = KIND == MKV_BF16 ? ptx::pack_bf16x2(p0, p1) : pack_f16x2(p0, p1);
+    }
+    tmem_st16(pT, pk);
+}
+// The row's weights 2^(s * mul + ref), over S in tensor memory; returns their sum.  The 16-bit weights of columns
+// c.. go to columns c / 2.., behind what is still to be read.
+template <int KIND, bool EDGE>
+__device__ inline float row_weights(uint32_t sT, float mul, float ref, int top, int bottom) {
+    const uint64_t m2 = pair(mul, mul), r2 = pair(ref, ref);
+    uint64_t sum[2] = {0, 0};
+    uint32_t x[32], y[32];
+    tmem_ld32(sT, x);
+#pragma unroll 1
+    for (int c = 0; c < kTile; c += 64) {
+        wait_ld();
+        tmem_ld32(sT + c + 32, y);
+        hide<EDGE>(x, c, top, bottom);
+        weights32<KIND>(x, sT + c / 2, m2, r2, sum);
+        wait_ld();
+        if (c + 64 < kTile) tmem_ld32(sT + c + 64, x);
+        hide<EDGE>(y, c + 32, top, bottom);
+        weights32<KIND>(y, sT + c / 2 + 16, m2, r2, sum);
+    }
+    const float2 s = unpair(add2(sum[0], sum[1]));
+    return s.x + s.y;
+}
+
 // ---- softmax threads: this thread's row of half w
 template <int KIND, int D, bool IO32>
 __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const Range& rg, uint32_t smem) {
     using C = TileCfg<D>;
-    const int tid = threadIdx.x, w = tid >> 7, row = tid & 127, warp4 = (tid >> 5) & 3;
+    const int tid = threadIdx.x, w = tid >> 7, row = tid & 127, warp4 = (tid >> 5) & 3, lane = tid & 31;
+    const int warp_row = (tid >> 5) * 32;   // first row of the warp, of the unit's 256
     const uint32_t lanes = (uint32_t)(warp4 * 32) << 16;
     const uint32_t sT = sh.tmem + lanes + w * 128, oT = sh.tmem + lanes + 256 + w * 128;
     const uint32_t q_full = ptx::smem_u32(&sh.q_full[w]), s_full = ptx::smem_u32(&sh.s_full[w]), p_full = ptx::smem_u32(&sh.p_full[w]),
                    o_full = ptx::smem_u32(&sh.o_full[w]);
+    const RowsOut rows_out{smem + C::kOut + (tid >> 5) * 8192, lane};
     const uint32_t q_smem = smem + w * C::kHalf, v_smem = smem + 4 * C::kHalf;
     uint32_t s_par = 0, o_par = 0;
     int tiles = 0;            // of this CTA so far: stage and parity of K and V
@@ -224,48 +354,57 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
         const bool live = r < u.rows;
         float m = -FLT_MAX, l = 0.f, back = a.scale_log2;
         if (nt > 0 && active) {
-            // ---- Q: this thread's row
-            if (KIND == MKV_BF16) {
-                const uint4* src = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + (place.at / a.c.q_heads) * a.q_stride + (place.at % a.c.q_heads) * D);
+            // ---- Q: the warp's 32 rows, D / 8 lanes for a row, all loads on their way before the first is used
+            constexpr int kPer = D / 8, kAt = 32 / kPer, kN = 32 / kAt;   // lanes of a row, rows at a time, times
+            const int c = lane % kPer;
+            constexpr int kWords = KIND == MKV_INT4 && IO32 ? 2 : 1;
+#pragma unroll 1
+            for (int i0 = 0; i0 < kN; i0 += 8) {
+            uint4 x[8][kWords];
 #pragma unroll
-                for (int c = 0; c < D / 8; ++c) {
-                    const uint4 x = live ? src[c] : make_uint4(0, 0, 0, 0);
-                    sts128(chunk_at(q_smem, row, c), x.x, x.y, x.z, x.w);
-                }
-            } else {
-                // fp16, scaled by a power of two to [2^13, 2^14); channels of eight in the order 0 4 1 5 2 6 3 7, as
-                // the codes' nibbles come (K has the same order)
-                const size_t at = (place.at / a.c.q_heads) * a.q_stride + (place.at % a.c.q_heads) * D;
-                float big = 0.f;
-                auto load8 = [&](int c, float (&x)[8]) {
+            for (int i = 0; i < 8; ++i) {
+                const int rr = (i0 + i) * kAt + lane / kPer;
+                const int tok = __shfl_sync(kFull, place.tok, rr), head = __shfl_sync(kFull, place.head, rr);
+                const bool in = warp_row + rr < u.rows;
+                const size_t at = (size_t)tok * a.q_stride + (size_t)head * D + 8 * c;
+#pragma unroll
+                for (int k = 0; k < kWords; ++k)
+                    x[i][k] = !in ? make_uint4(0, 0, 0, 0)
+                              : kWords == 2 ? __ldg(reinterpret_cast<const uint4*>((const float*)a.q + at) + k)
+                                            : __ldg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + at));
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int rr = (i0 + i) * kAt + lane / kPer, row16 = warp4 * 32 + rr;
+                if (KIND == MKV_BF16) {
+                    sts128(chunk_at(q_smem, row16, c), x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w);
+                } else {
+                    // fp16, scaled by a power of two to [2^13, 2^14); channels of eight in the order 0 4 1 5 2 6 3 7, as
+                    // the codes' nibbles come (K has the same order)
+                    float y[8];
                     if (IO32) {
-                        const float4 v0 = reinterpret_cast<const float4*>((const float*)a.q + at)[2 * c], v1 = reinterpret_cast<const float4*>((const float*)a.q + at)[2 * c + 1];
-                        x[0] = v0.x; x[1] = v0.y; x[2] = v0.z; x[3] = v0.w; x[4] = v1.x; x[5] = v1.y; x[6] = v1.z; x[7] = v1.w;
+                        const uint4 p0 = x[i][0], p1 = x[i][kWords - 1];
+                        y[0] = __uint_as_float(p0.x); y[1] = __uint_as_float(p0.y); y[2] = __uint_as_float(p0.z); y[3] = __uint_as_float(p0.w);
+                        y[4] = __uint_as_float(p1.x); y[5] = __uint_as_float(p1.y); y[6] = __uint_as_float(p1.z); y[7] = __uint_as_float(p1.w);
                     } else {
-                        const uint4 v = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + at)[c];
-                        const uint32_t z[4] = {v.x, v.y, v.z, v.w};
+                        const uint32_t z[4] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w};
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) { x[2 * e] = __uint_as_float(z[e] << 16); x[2 * e + 1] = __uint_as_float(z[e] & 0xffff0000u); }
+                        for (int e = 0; e < 4; ++e) { y[2 * e] = __uint_as_float(z[e] << 16); y[2 * e + 1] = __uint_as_float(z[e] & 0xffff0000u); }
                     }
-                };
-#pragma unroll 4
-                for (int c = 0; c < D / 8; ++c) {
-                    float x[8];
-                    load8(c, x);
+                    float big = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(x[e]));
+                    for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(y[e]));
+#pragma unroll
+                    for (int o = kPer / 2; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(kFull, big, o));
+                    const int ex = min(max((int)(__float_as_uint(big) >> 23), 16), 254);
+                    const float up = __uint_as_float((uint32_t)min(254, 127 + 13 + 127 - ex) << 23);
+                    sts128(chunk_at(q_smem, row16, c), pack_f16x2(y[0] * up, y[4] * up), pack_f16x2(y[1] * up, y[5] * up),
+                           pack_f16x2(y[2] * up, y[6] * up), pack_f16x2(y[3] * up, y[7] * up));
+                    // back to the row's own thread
+                    const float mine = __shfl_sync(kFull, up, (lane % kAt) * kPer);
+                    if (lane / kAt == i0 + i) back = a.scale_log2 * (1.f / mine);
                 }
-                const int ex = min(max((int)(__float_as_uint(big) >> 23), 16), 254);
-                const float up = __uint_as_float((uint32_t)min(254, 127 + 13 + 127 - ex) << 23);
-                back = a.scale_log2 * (1.f / up);
-#pragma unroll 4
-                for (int c = 0; c < D / 8; ++c) {
-                    float x[8];
-                    load8(c, x);
-                    const float z = live ? up : 0.f;
-                    sts128(chunk_at(q_smem, row, c), live ? pack_f16x2(x[0] * z, x[4] * z) : 0u, live ? pack_f16x2(x[1] * z, x[5] * z) : 0u,
-                           live ? pack_f16x2(x[2] * z, x[6] * z) : 0u, live ? pack_f16x2(x[3] * z, x[7] * z) : 0u);
-                }
+            }
             }
             ptx::fence_proxy_async();
             ptx::mbar_arrive(q_full);
@@ -286,20 +425,27 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                     const bool some = !none && (p > u.plo || (a.window > 0 && p <= u.phi - a.window));
                     if (none || some) {
                         bool odd = false;
-#pragma unroll 4
-                        for (int i = 0; i < D / 8; ++i) {
-                            const uint32_t at = chunk_at(v_smem + stage * C::kHalf, row, (i & 8) | ((i + row) & 7));
-                            if (none) { sts128(at, 0, 0, 0, 0); continue; }
-                            uint32_t x[4];
-                            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at));
-                            bool hit = false;
+#pragma unroll 1
+                        for (int i0 = 0; i0 < D / 8; i0 += 8) {
+                            // eight chunks of the row, in an order that keeps the warp's lanes in different banks
+                            uint4 x[8];
+                            if (!none) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                if ((x[e] & 0x7f80u) == 0x7f80u) { x[e] &= 0xffff0000u; hit = true; }
-                                if ((x[e] & 0x7f800000u) == 0x7f800000u) { x[e] &= 0xffffu; hit = true; }
+                                for (int i = 0; i < 8; ++i) x[i] = lds128(chunk_at(v_smem + stage * C::kHalf, row, i0 + ((i + row) & 7)));
                             }
-                            if (hit) sts128(at, x[0], x[1], x[2], x[3]);
-                            odd |= hit;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const uint32_t at = chunk_at(v_smem + stage * C::kHalf, row, i0 + ((i + row) & 7));
+                                if (none) { sts128(at, 0, 0, 0, 0); continue; }
+                                bool hit = false;
+                                auto look = [&](uint32_t& z) {
+                                    if ((z & 0x7f80u) == 0x7f80u) { z &= 0xffff0000u; hit = true; }
+                                    if ((z & 0x7f800000u) == 0x7f800000u) { z &= 0xffffu; hit = true; }
+                                };
+                                look(x[i].x); look(x[i].y); look(x[i].z); look(x[i].w);
+                                if (hit) sts128(at, x[i].x, x[i].y, x[i].z, x[i].w);
+                                odd |= hit;
+                            }
                         }
                         if (odd) {
                             sh.odd[atomicAdd(&sh.n_odd, 1) % kOddMax] = make_int2(tiles + j, p);
@@ -317,19 +463,7 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                     f = sh.v_exp[stage];
                 }
                 const int top = place.pos - t0, bottom = a.window > 0 ? top - a.window : INT_MIN;   // bottom < column <= top
-                uint32_t v[32];
-                float mx = kPagedNegInf;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    tmem_ld32(sT + 32 * c, v);
-                    wait_ld();
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        float s = __uint_as_float(v[e]);
-                        if (edge && (32 * c + e > top || 32 * c + e <= bottom)) s = kPagedNegInf;
-                        mx = fmaxf(mx, s);
-                    }
-                }
+                float mx = edge ? row_max<true>(sT, top, bottom) : row_max<false>(sT, 0, 0);
                 mx = fmaf(mx, mul, f);
                 const bool move = mx > m + 8.f;
                 if (__any_sync(kFull, move)) {
@@ -339,6 +473,7 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                     if (j > 0) {   // the products before are complete: this tile's S was issued behind them
 #pragma unroll 1
                         for (int c = 0; c < D / 32; ++c) {
+                            uint32_t v[32];
                             tmem_ld32(oT + 32 * c, v);
                             wait_ld();
 #pragma unroll
@@ -349,25 +484,7 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                     }
                 }
                 const float ref = f - m;
-                float sum = 0.f;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    tmem_ld32(sT + 32 * c, v);
-                    wait_ld();
-                    uint32_t pk[16];
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        float s0 = __uint_as_float(v[e]), s1 = __uint_as_float(v[e + 1]);
-                        if (edge) {
-                            if (32 * c + e > top || 32 * c + e <= bottom) s0 = kPagedNegInf;
-                            if (32 * c + e + 1 > top || 32 * c + e + 1 <= bottom) s1 = kPagedNegInf;
-                        }
-                        const float p0 = ex2(fmaf(s0, mul, ref)), p1 = ex2(fmaf(s1, mul, ref));
-                        sum += p0 + p1;
-                        pk[e >> 1] = KIND == MKV_BF16 ? ptx::pack_bf16x2(p0, p1) : pack_f16x2(p0, p1);
-                    }
-                    tmem_st16(sT + 16 * c, pk);
-                }
+                const float sum = edge ? row_weights<KIND, true>(sT, mul, ref, top, bottom) : row_weights<KIND, false>(sT, mul, ref, 0, 0);
                 l += KIND == MKV_INT4 ? sum * ex2(-f) : sum;
                 wait_st();
                 fence_before();
@@ -382,6 +499,7 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
         if (any_leaves(!ok)) return;   // and the list of odd tokens is complete
         // ---- the row's result, or its part
         const bool whole = lo == u.base && hi == u.end();
+        uint8_t* const out_row = live ? (uint8_t*)a.out + place.at * (D * (a.c.out_f32 ? 4 : 2)) : nullptr;
         const TilePart part = tile_part<D>(a, 2 * blockIdx.x + (rg.t0 < u.base ? 1 : 0));
         if (active) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -413,13 +531,11 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                         }
                     }
                 }
-                if (!live) continue;
                 if (whole) {
-                    store32<D>(a, place.at, 32 * c, o, inv);
-                } else {
-                    float4* p = reinterpret_cast<float4*>(part.o + (size_t)r * D + 32 * c);
+                    store32<D>(a, rows_out, out_row, 32 * c, o, inv);
+                } else if (live) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) p[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    for (int i = 0; i < 8; ++i) *part.at(r, 32 * c + 4 * i) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                 }
             }
             fence_before();
@@ -438,34 +554,35 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                 __threadfence();
             }
             soft_barrier();
-            if (sh.last && live) {
+            if (sh.last && active) {
                 const int slot0 = 2 * c0 + (rg.begin_of(c0) < u.base ? 1 : 0);
+                // two passes over the parts: the common reference, then the sums; four parts' loads on their way at a time
                 float mm = -FLT_MAX, ll = 0.f;
-                for (int x = c0; x <= c1; ++x) mm = fmaxf(mm, __ldcg(tile_part<D>(a, x == c0 ? slot0 : 2 * x).m + r));
-                for (int x = c0; x <= c1; ++x) {
-                    const TilePart p = tile_part<D>(a, x == c0 ? slot0 : 2 * x);
-                    ll = fmaf(__ldcg(p.l + r), ex2(__ldcg(p.m + r) - mm), ll);
-                }
+                auto part_of = [&](int x) { return tile_part<D>(a, x == c0 ? slot0 : 2 * x); };
+#pragma unroll 4
+                for (int x = c0; x <= c1; ++x) mm = fmaxf(mm, __ldcg(part_of(x).m + r));
+#pragma unroll 4
+                for (int x = c0; x <= c1; ++x) ll = fmaf(__ldcg(part_of(x).l + r), ex2(__ldcg(part_of(x).m + r) - mm), ll);
                 const float inv = ll == 0.f ? 0.f : 1.f / ll;
 #pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
                     float o[32];
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = 0.f;
+#pragma unroll 2
                     for (int x = c0; x <= c1; ++x) {
-                        const TilePart p = tile_part<D>(a, x == c0 ? slot0 : 2 * x);
+                        const TilePart p = part_of(x);
                         const float sc = ex2(__ldcg(p.m + r) - mm);
-                        const float4* y = reinterpret_cast<const float4*>(p.o + (size_t)r * D + 32 * c);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            const float4 z = __ldcg(y + i);
+                            const float4 z = __ldcg(p.at(r, 32 * c + 4 * i));
                             o[4 * i] = fmaf(z.x, sc, o[4 * i]); o[4 * i + 1] = fmaf(z.y, sc, o[4 * i + 1]);
                             o[4 * i + 2] = fmaf(z.z, sc, o[4 * i + 2]); o[4 * i + 3] = fmaf(z.w, sc, o[4 * i + 3]);
                         }
                     }
-                    store32<D>(a, place.at, 32 * c, o, inv);
+                    store32<D>(a, rows_out, out_row, 32 * c, o, inv);
                 }
-                if (a.lse) a.lse[place.at] = ll == 0.f ? kPagedNegInf : (mm + log2f(ll)) * 0.69314718055994531f;
+                if (live && a.lse) a.lse[place.at] = ll == 0.f ? kPagedNegInf : (mm + log2f(ll)) * 0.69314718055994531f;
             }
         }
         if (u.end() >= rg.t1 || !next_unit<kRows, kTile>(a, u)) return;
@@ -577,8 +694,8 @@ __device__ inline void copy_role(const PagedAttendArgs& a, Shared& sh, const Ran
     // the CTA must not end with copies on their way: they are waited for by the products, except after a wait that ran out
     if (*(volatile int*)&sh.dead)
         for (int k = max(0, tiles - 2); k <= tiles; ++k) {
-            ptx::mbar_wait_bounded(ptx::smem_u32(&sh.k_full[k & 1]), (k >> 1) & 1, kWaitNs / 8);
-            ptx::mbar_wait_bounded(ptx::smem_u32(&sh.v_full[k & 1]), (k >> 1) & 1, kWaitNs / 8);
+            paged_wait(ptx::smem_u32(&sh.k_full[k & 1]), (k >> 1) & 1);
+            paged_wait(ptx::smem_u32(&sh.v_full[k & 1]), (k >> 1) & 1);
         }
 }
 

@@ -3,8 +3,22 @@
 // the device, so every CTA sums them for itself.
 #pragma once
 #include "mkv_paged.cuh"
+#include "mkv_ptx.cuh"
 
 namespace mkv {
+
+// Bounded wait, for a few seconds at most.  The limit is counted in cycles: reading the global timer takes longer than
+// most waits do (the kernel for many rows ran KTIME with it).
+__device__ inline bool paged_wait(uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < 16; ++i)
+        if (ptx::mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    do {
+        for (int i = 0; i < 64; ++i)
+            if (ptx::mbar_try_wait(bar, parity)) return true;
+    } while (clock64() - t0 < (1ll << 32));
+    return false;
+}
 
 // One (sequence, KV head, row tile), and the part of the block list that is its own.
 struct Unit {
