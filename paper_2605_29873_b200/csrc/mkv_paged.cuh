@@ -120,7 +120,6 @@ __device__ inline float paged_bf16(uint32_t bits16) { return __uint_as_float(bit
 
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int head_dim, cudaStream_t st);
 cudaError_t launch_paged_read(const PagedReadArgs& a, int head_dim, cudaStream_t st);
-cudaError_t launch_paged_simt(const PagedAttendArgs& a, int head_dim, cudaStream_t st);
 size_t paged_decode_scratch();   // workspace of launch_paged_decode, zero before its first launch
 bool make_paged_map(void* map, const void* pages, long long rows, int head_dim, int box_rows);   // bf16 pages as one list of rows
 cudaError_t launch_paged_decode(const PagedAttendArgs& a, int head_dim, const void* map, long long layer_rows, int sm_count,

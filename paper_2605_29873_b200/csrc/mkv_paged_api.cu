@@ -203,8 +203,9 @@ mkv_status mkv_paged_attend(mkv_paged* c, int layer, const void* q, int64_t q_st
     a.scratch = c->ws + paged_ws().scratch;
     const long long rows_per_layer = (long long)c->n_pages * 2 * c->kv_heads * c->page_size;
     const cudaStream_t st = (cudaStream_t)stream;
-    const cudaError_t e = c->kv_dtype == MKV_F32 ? launch_paged_simt(a, c->head_dim, st)
-                          : (long long)a.c.group * a.max_new <= 64
+    // Few rows of a sequence and head: the cache is streamed, a unit's rows on one pass.  Many: tiles on the tensor
+    // cores.  fp32 pages have the first form only.
+    const cudaError_t e = c->kv_dtype == MKV_F32 || (long long)a.c.group * a.max_new <= 64
                               ? launch_paged_decode(a, c->head_dim, &c->map16, layer * rows_per_layer, c->sm_count, st)
                               : launch_paged_tile(a, c->head_dim, &c->map_page, layer * rows_per_layer, c->sm_count, st);
     if (e != cudaSuccess) return MKV_ERR_CUDA;

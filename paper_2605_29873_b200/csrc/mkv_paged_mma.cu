@@ -26,7 +26,10 @@
 //       applied to their fp32 sums, the second term one more matrix product with sum(q) as three bf16
 //   O = sum_t codes_t (p_t scale_t) + lowest_t p_t          p * scale in fp16 per group; lowest again
 //       one more product, p as two bf16
-// q enters as fp16 scaled by a power of two to the top of its range: exact for bf16 queries down to
+// fp32 pages: scalar arithmetic in the same frame (for 8 rows it needs a third of the issue slots that HBM leaves).  A
+// lane holds its channels of all rows' q and O; the 32 sums of 8 rows x 4 tokens are added across the lanes
+// by exchanging halves (31 shuffles), after which every lane has one of them.
+// q over 4-bit pages enters as fp16 scaled by a power of two to the top of its range: exact for bf16 queries down to
 // 2^-24 of a row's largest; fp32 queries as a sum of two fp16 in the unused half of the 16 rows.
 // p * scale is kept within fp16 by moving m with log2 of the block's largest scale: rounding 2^-12 of
 // each weight, below what a bf16 result shows; with fp32 results it enters as the sum of two fp16.
@@ -49,14 +52,15 @@ constexpr unsigned kFull = 0xffffffffu;
 template <int KIND, int D, int NT>
 struct Cfg {
     static constexpr int RT = 8 * NT;
-    static constexpr int kStage = KIND == MKV_INT4 ? 16 * D + 128 * (D / 32) : 16 * D * 4;
+    static constexpr int kStage = KIND == MKV_INT4 ? 16 * D + 128 * (D / 32) : 16 * D * (KIND == MKV_F32 ? 8 : 4);
     // bytes in flight per SM want 44 KB (6.5 TB/s x 1 us / 148): three stages of eight warps, of which one is read
-    static constexpr int kStages = KIND == MKV_INT4 || NT == 1 ? 3 : 2;
+    static constexpr int kStages = KIND == MKV_F32 && D == 128 ? 1 : KIND == MKV_INT4 || NT == 1 ? 3 : 2;
     static constexpr int DP = D + 4;
     static constexpr int kRing = kW * kStages * kStage;
     static constexpr int kMerge = kW * RT * DP * 4;
     static constexpr int kMl = kW * RT * 8;
-    static constexpr int kSmem = 1024 + kRing + kMerge + kMl;
+    static constexpr int kWeights = KIND == MKV_F32 ? kW * 16 * 8 * 4 : 0;   // a block's p [token][row] per warp
+    static constexpr int kSmem = 1024 + kRing + kMerge + kMl + kWeights;
 };
 
 __device__ inline float ex2(float x) {
@@ -537,6 +541,123 @@ __device__ inline void block_int4(State<D, NT>& st, const QInt4<D, NT, Q32>& q, 
     }
 }
 
+// ---- fp32 pages
+
+// Lane: channels lane * CPL .. of every row; of the softmax, row lane & 7.
+template <int D>
+struct StateF32 {
+    static constexpr int CPL = D / 32;
+    float m[1], l[1];
+    float o[8][CPL];
+};
+template <int D> struct QF32 { float q[8][D / 32]; };
+
+template <int N> __device__ inline void lds_floats(uint32_t addr, float (&x)[N]) {
+    if (N == 4) asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[N > 2 ? 2 : 0]), "=f"(x[N > 2 ? 3 : 0]) : "r"(addr));
+    else asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(x[0]), "=f"(x[1]) : "r"(addr));
+}
+
+template <int D>
+__device__ inline void load_q(const PagedAttendArgs& a, const Unit& u, QF32<D>& q, int lane) {
+    constexpr int CPL = D / 32;
+    const int G = a.c.group;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        const int row = u.row0 + min(r, u.rows - 1), j = row / G;
+        const float* p = (const float*)a.q + (size_t)(u.tok0 + j) * a.q_stride + (size_t)(u.h * G + row - j * G) * D + lane * CPL;
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) q.q[r][e] = p[e] * a.scale_log2;
+    }
+}
+
+template <int D, bool EDGE>
+__device__ inline void block_f32(StateF32<D>& st, const QF32<D>& q, const PagedAttendArgs& a, const Unit& u, int pos, uint32_t stage,
+                                 uint32_t weights, int tok, int lane) {
+    constexpr int CPL = D / 32;
+    float s[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        float x[32];   // row + 8 * token
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            float k[CPL];
+            lds_floats<CPL>(stage + (4 * b + t) * (D * 4) + lane * (CPL * 4), k);
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                float y = q.q[r][0] * k[0];
+#pragma unroll
+                for (int e = 1; e < CPL; ++e) y = fmaf(q.q[r][e], k[e], y);
+                x[8 * t + r] = y;
+            }
+        }
+#pragma unroll
+        for (int h = 16; h; h >>= 1) {
+            const bool up = lane & h;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (i < h) {
+                    const float keep = up ? x[i + h] : x[i], give = up ? x[i] : x[i + h];
+                    x[i] = keep + __shfl_xor_sync(kFull, give, h);
+                }
+        }
+        s[b] = x[0];   // row lane & 7, token 4 b + lane / 8
+        if (EDGE) {
+            const int p = tok + 4 * b + (lane >> 3);
+            if (p > pos || (a.window > 0 && p <= pos - a.window)) s[b] = kPagedNegInf;
+        }
+    }
+    float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    if (__any_sync(kFull, mx > st.m[0] + 8.f)) {
+        mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, 8));
+        mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, 16));
+        const float m = fmaxf(st.m[0], mx), sc = ex2(st.m[0] - m);
+        st.m[0] = m;
+        st.l[0] *= sc;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const float f = __shfl_sync(kFull, sc, r);
+#pragma unroll
+            for (int e = 0; e < CPL; ++e) st.o[r][e] *= f;
+        }
+    }
+    __syncwarp();   // the weights before have been read
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const float p = ex2(s[b] - st.m[0]);
+        st.l[0] += p;
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(weights + (32 * b + lane) * 4), "f"(p) : "memory");
+    }
+    __syncwarp();
+    const int first = a.window > 0 ? u.plo - a.window + 1 : 0;
+#pragma unroll 4
+    for (int t = 0; t < 16; ++t) {
+        if (EDGE && (tok + t > u.phi || tok + t < first)) continue;   // rows that nobody sees may hold anything
+        float v[CPL], p[2][4];
+        lds_floats<CPL>(stage + 16 * D * 4 + t * (D * 4) + lane * (CPL * 4), v);
+        lds_floats<4>(weights + t * 32, p[0]);
+        lds_floats<4>(weights + t * 32 + 16, p[1]);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            if (EDGE && p[r >> 2][r & 3] == 0.f) continue;   // nor may a NaN meet the weight of a row that does not see it
+#pragma unroll
+            for (int e = 0; e < CPL; ++e) st.o[r][e] = fmaf(p[r >> 2][r & 3], v[e], st.o[r][e]);
+        }
+    }
+}
+
+template <int D>
+__device__ inline void put_state(StateF32<D>& st, float* o, float2* ml, int lane) {
+    constexpr int DP = D + 4, CPL = D / 32;
+    float l = st.l[0];
+    l += __shfl_xor_sync(kFull, l, 8);
+    l += __shfl_xor_sync(kFull, l, 16);
+    if (lane < 8) ml[lane] = make_float2(st.m[0], l);
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) o[r * DP + lane * CPL + e] = st.o[r][e];
+}
+
 // A warp's state into its slot of the merge buffer: O [RT][D + 4], and (m, l) per row.
 template <int KIND, int D, int NT>
 __device__ inline void put_state(State<D, NT>& st, float* o, float2* ml, int lane) {
@@ -569,6 +690,28 @@ __device__ inline void put_state(State<D, NT>& st, float* o, float2* ml, int lan
             }
         }
     }
+}
+
+template <int D, int NT>
+__device__ inline void clear(State<D, NT>& st) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        st.m[i] = -FLT_MAX; st.l[i] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            st.lowest[i][e] = 0.f;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) st.o[k][i][e] = 0.f;
+        }
+    }
+}
+template <int D>
+__device__ inline void clear(StateF32<D>& st) {
+    st.m[0] = -FLT_MAX; st.l[0] = 0.f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) st.o[r][e] = 0.f;
 }
 
 template <int KIND, int D, int NT, bool Q32, bool HL>
@@ -632,6 +775,10 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
             if (KIND == MKV_INT4) {
                 ptx::bulk_g2s(dst, a.c.pages + (size_t)page * a.c.page_bytes + (size_t)f.h * a.c.head_bytes + (size_t)(row >> 4) * C::kStage,
                               C::kStage, bar);
+            } else if (KIND == MKV_F32) {
+                const uint8_t* src = a.c.pages + (size_t)page * a.c.page_bytes + (size_t)f.h * a.c.head_bytes + (size_t)row * (D * 4);
+                ptx::bulk_g2s(dst, src, C::kStage / 2, bar);
+                ptx::bulk_g2s(dst + C::kStage / 2, src + a.c.kv_bytes, C::kStage / 2, bar);
             } else {
                 const int kv = a.c.kv_heads << a.c.page_shift;
                 const int y = (int)(layer_rows + (long long)page * 2 * kv) + (f.h << a.c.page_shift) + row;
@@ -651,7 +798,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
     for (int i = 0; i < C::kStages; ++i) fetch();
 
     // ---- units of the range
-    State<D, NT> st;
+    typename std::conditional<KIND == MKV_F32, StateF32<D>, State<D, NT>>::type st;
     int stage = 0, parity = 0;
     bool ok = true;
     for (;;) {
@@ -660,17 +807,12 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
         int pos[NT];
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-            pos[i] = u.len - u.n + (u.row0 + min((lane >> 2) + 8 * i, u.rows - 1)) / a.c.group;
-            st.m[i] = -FLT_MAX; st.l[i] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                st.lowest[i][e] = 0.f;
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) st.o[k][i][e] = 0.f;
-            }
+            const int row = KIND == MKV_F32 ? lane & 7 : (lane >> 2) + 8 * i;
+            pos[i] = u.len - u.n + (u.row0 + min(row, u.rows - 1)) / a.c.group;
         }
+        clear(st);
         if (warp < cnt) {
-            typename std::conditional<KIND == MKV_INT4, QInt4<D, NT, Q32>, QBf16<D, NT>>::type q;
+            typename std::conditional<KIND == MKV_INT4, QInt4<D, NT, Q32>, typename std::conditional<KIND == MKV_F32, QF32<D>, QBf16<D, NT>>::type>::type q;
             load_q(a, u, q, lane);
             for (int i = warp; i < cnt; i += kW) {
                 if (ok && !paged_wait(bar0 + stage * 8, parity)) {
@@ -685,6 +827,10 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
                 if constexpr (KIND == MKV_INT4) {
                     if (edge) block_int4<D, NT, Q32, HL, true>(st, q, a, u, pos, at, tok, lane);
                     else block_int4<D, NT, Q32, HL, false>(st, q, a, u, pos, at, tok, lane);
+                } else if constexpr (KIND == MKV_F32) {
+                    const uint32_t weights = ptx::smem_u32(smem) + C::kRing + C::kMerge + C::kMl + warp * 512;
+                    if (edge) block_f32<D, true>(st, q, a, u, pos[0], at, weights, tok, lane);
+                    else block_f32<D, false>(st, q, a, u, pos[0], at, weights, tok, lane);
                 } else {
                     if (edge) block_bf16<D, NT, true>(st, q, a, u, pos, at, tok, lane);
                     else block_bf16<D, NT, false>(st, q, a, u, pos, at, tok, lane);
@@ -695,7 +841,8 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
                 fetch();
             }
         }
-        put_state<KIND, D, NT>(st, merge + warp * RT * DP, mls + warp * RT, lane);
+        if constexpr (KIND == MKV_F32) put_state<D>(st, merge + warp * RT * DP, mls + warp * RT, lane);
+        else put_state<KIND, D, NT>(st, merge + warp * RT * DP, mls + warp * RT, lane);
         __syncthreads();
         // ---- the warps' states become one
         const bool whole = lo == u.base && hi == u.end();
@@ -801,6 +948,7 @@ cudaError_t launch_paged_decode(const PagedAttendArgs& a, int D, const void* map
 #define MKV_GO(KIND, NT, Q32, HL)                                                                  \
     return D == 128 ? decode_t<KIND, 128, NT, Q32, HL>(a, m, layer_rows, sm_count, st)             \
                     : decode_t<KIND, 64, NT, Q32, HL>(a, m, layer_rows, sm_count, st)
+    if (a.c.kv_dtype == MKV_F32) { MKV_GO(MKV_F32, 1, false, false); }
     if (a.c.kv_dtype == MKV_BF16) {
         if (one) { MKV_GO(MKV_BF16, 1, false, false); }
         MKV_GO(MKV_BF16, 2, false, false);
