@@ -1,6 +1,8 @@
 // Writing the paged cache (with the rotation of keys and queries on the way) and reading its rows
 // back as values.  Elementwise work: bound by memory for prompts, by the latency of a launch and
 // three dependent loads (starts, lens, table) for single tokens.
+#include <cfloat>
+
 #include "mkv_paged.cuh"
 
 namespace mkv {
@@ -82,163 +84,299 @@ __device__ inline double turn_fraction(int pos, float inv_freq) {
     return 2.0 * (turns - rint(turns));
 }
 
-// One quantised piece: the four channels 4 * l .. 4 * l + 3 of a head, lanes of eight sharing a
-// group.  In 64 bits up to the code, so that a value next to a border between two codes goes where
-// the definition sends it.
-struct Coded { uint32_t codes16; uint16_t scale, lowest; };
-__device__ inline Coded quantise4(const double (&x)[4]) {
-    double lo = fmin(fmin(x[0], x[1]), fmin(x[2], x[3])), hi = fmax(fmax(x[0], x[1]), fmax(x[2], x[3]));
-    // fmin / fmax pass over a NaN, so finiteness is looked at apart
-    int fine = isfinite(x[0]) && isfinite(x[1]) && isfinite(x[2]) && isfinite(x[3]);
+// One quantised piece: eight channels of a head, lanes of four sharing a group.
+struct Coded { uint32_t codes; uint16_t scale, lowest; };
+
+// In 64 bits up to the code, so that a value next to a border between two codes goes where the
+// definition sends it.
+__device__ __noinline__ Coded quantise8_wide(const double (&x)[8]) {
+    double lo = x[0], hi = x[0];
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
+    for (int i = 1; i < 8; ++i) { lo = fmin(lo, x[i]); hi = fmax(hi, x[i]); }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
         lo = fmin(lo, __shfl_xor_sync(0xffffffffu, lo, o));
         hi = fmax(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-        fine &= __shfl_xor_sync(0xffffffffu, fine, o);
     }
     Coded r;
-    r.codes16 = 0;
-    if (!fine) { r.scale = 0x7fc0; r.lowest = 0; return r; }
+    r.codes = 0;
     const __nv_bfloat16 sb = __float2bfloat16_rn((float)(hi / 15.0 - lo / 15.0)), lb = __float2bfloat16_rn((float)lo);
     r.scale = __bfloat16_as_ushort(sb);
     r.lowest = __bfloat16_as_ushort(lb);
     const double s = (double)__bfloat162float(sb), l = (double)__bfloat162float(lb);
     if (s > 0.0) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 8; ++i) {
             const double n = fmin(15.0, fmax(0.0, rint((x[i] - l) / s)));
-            r.codes16 |= (uint32_t)n << (4 * i);
+            r.codes |= (uint32_t)n << (4 * i);
         }
     }
     return r;
 }
 
-// TT tokens per CTA.  KIND: the cache's mkv_dtype.
+__device__ inline float min_nan(float a, float b) { float y; asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
+__device__ inline float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
+
+// The same in 32 bits, where that decides it: x[i] is within err[i] of the exact value (short16: is a bf16).  *unsure: some
+// rounding (of the scale, the lowest value, a code) could go either way; the warp then takes the 64-bit
+// form (about one rotated group in a thousand).
+__device__ inline Coded quantise8(const float (&x)[8], const float (&err)[8], bool short16, bool* unsure) {
+    float lo = x[0], hi = x[0], e = err[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) { lo = min_nan(lo, x[i]); hi = max_nan(hi, x[i]); e = fmaxf(e, err[i]); }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        e = fmaxf(e, __shfl_xor_sync(0xffffffffu, e, o));
+    }
+    Coded r;
+    const float t = hi * (1.f / 15.f) - lo * (1.f / 15.f);
+    const float te = e * (2.f / 15.f) + (fabsf(hi) + fabsf(lo)) * 1.5e-8f + t * 1.2e-7f;   // 1/15 and its products are 2^-23 off at most
+    const __nv_bfloat16 sb = __float2bfloat16_rn(t), lb = __float2bfloat16_rn(lo);
+    bool u = __bfloat16_as_ushort(__float2bfloat16_rn(t - te)) != __bfloat16_as_ushort(__float2bfloat16_rn(t + te)) ||
+             __bfloat16_as_ushort(__float2bfloat16_rn(lo - e)) != __bfloat16_as_ushort(__float2bfloat16_rn(lo + e)) ||
+             t < 1e-35f;   // and scales whose reciprocal or differences leave the normal range
+    r.scale = __bfloat16_as_ushort(sb);
+    r.lowest = __bfloat16_as_ushort(lb);
+    const float s = __bfloat162float(sb), l = __bfloat162float(lb), inv = __frcp_rn(s);
+    r.codes = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        // k = floor((x - l) / s), or one less or more where that is next to a whole number; then on which side of
+        // (k + 1/2) s, an exact product, x - l lies.  1.5 * 2^23 puts k into the lowest bits.
+        constexpr float kOne = 12582912.f;
+        const float d = x[i] - l;
+        const float k = fminf(fmaxf(fmaf(d, inv, -0.5f) + kOne, kOne), kOne + 14.f);
+        const float rest = fmaf(-((k - kOne) + 0.5f), s, d);
+        uint32_t code = __float_as_uint(k) & 15u;
+        if (rest > 0.f) code += 1;
+        if (fabsf(rest) <= fabsf(d) * 1.2e-7f) {
+            // on the border, as far as the difference is exact: that of two bf16 is, unless their sizes are far apart.  A
+            // tie goes to the even code.
+            if (rest == 0.f) code += code & 1u;
+            const float big = fmaxf(fabsf(x[i]), fabsf(l)), small = fminf(fabsf(x[i]), fabsf(l));
+            u |= !short16 || (small != 0.f && small * 16384.f < big);
+        }
+        u |= fabsf(rest) < err[i];
+        r.codes |= code << (4 * i);
+    }
+    *unsure = u;
+    if (!(fabsf(lo) <= FLT_MAX && fabsf(hi) <= FLT_MAX)) { r.codes = 0; r.scale = 0x7fc0; r.lowest = 0; *unsure = false; }
+    return r;
+}
+
+// cos and sin of a token's pairs, in the order in which a thread takes them: eight pairs (an item) as four 16-byte
+// pieces, the pieces of all items next to one another.
+template <int D> __device__ inline int cs_at(int pair) { return ((pair >> 1) & 3) * (D / 8) + (pair >> 3) * 2 + (pair & 1); }
+
+// In 64 bits: eight channels from c on of a row, rotated where `turn`.
+template <typename T>
+__device__ __noinline__ Coded code_wide(const T* src, int c, bool turn, int rot_pos, const float* inv_freq, int half, int interleaved) {
+    double d[8];
+    const bool up = c >= half;
+#pragma unroll 1
+    for (int e = 0; e < 8; ++e) {
+        d[e] = (double)(float)src[c + e];
+        if (turn) {
+            const int pair = interleaved ? (c + e) >> 1 : up ? c + e - half : c + e;
+            const double p = (double)(float)src[interleaved ? (c + e) ^ 1 : up ? c + e - half : c + e + half];
+            double sn, cn;
+            sincospi(turn_fraction(rot_pos, inv_freq[pair]), &sn, &cn);
+            d[e] = (interleaved ? (e & 1) : up) ? d[e] * cn + p * sn : d[e] * cn - p * sn;
+        }
+    }
+    return quantise8_wide(d);
+}
+
+// TT tokens per CTA.  KIND: the cache's mkv_dtype.  4-bit caches: blockIdx.y = 1 are the queries' blocks.
 template <typename T, int KIND, int D, int TT>
-__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const PagedAppendArgs a) {
+__global__ void __launch_bounds__(kAppendThreads, KIND == MKV_INT4 ? 3 : 5) paged_append_kernel(const PagedAppendArgs a) {
     __shared__ TokenPlace place[TT];
-    __shared__ float2 cs[TT][D / 2];
-    __shared__ double2 csd[KIND == MKV_INT4 ? TT : 1][KIND == MKV_INT4 ? D / 2 : 1];
+    __shared__ int pairs[TT];
+    __shared__ __align__(16) float2 cs[TT][D / 2];
     const int tid = threadIdx.x, tok0 = blockIdx.x * TT;
     if (tid < TT && tok0 + tid < a.b.n_tokens) place[tid] = token_place(a, tok0 + tid);
     else if (tid < TT) place[tid].skip = 1;
     __syncthreads();
     const int half = a.rot_dim >> 1;
-    for (int i = tid; i < TT * half; i += kAppendThreads) {
-        const int t = i / half, f = i - t * half;
-        if (place[t].skip) continue;
+    if (KIND == MKV_INT4 && TT > 1 && tid < TT) {
+        // tokens whose rows make a pair are stored together: 2 with the next, 0 with the one before, 1 alone
+        auto both = [&](int t) {
+            return t >= 0 && t + 1 < TT && !place[t].skip && !place[t + 1].skip && place[t].page && place[t].page == place[t + 1].page &&
+                   (place[t].row & 1) == 0 && place[t + 1].row == place[t].row + 1;
+        };
+        pairs[tid] = both(tid) ? 2 : both(tid - 1) ? 0 : 1;
+    }
+    for (int i = tid; i < TT * (D / 2); i += kAppendThreads) {
+        const int t = i / (D / 2), f = i % (D / 2);
+        if (f >= half || place[t].skip) continue;
+        // the fraction of a turn rounded to 32 bits, and what was left of it as a small further turn
         const double x = turn_fraction(place[t].rot_pos, a.inv_freq[f]);
-        if (KIND == MKV_INT4) {
-            double sd, cd;
-            sincospi(x, &sd, &cd);
-            csd[t][f] = make_double2(cd, sd);
-            cs[t][f] = make_float2((float)cd, (float)sd);
-        } else {
-            float sf, cf;
-            sincospif((float)x, &sf, &cf);
-            cs[t][f] = make_float2(cf, sf);
-        }
+        const float xf = (float)x, rest = (float)(x - (double)xf) * 3.14159265f;
+        float sf, cf;
+        sincospif(xf, &sf, &cf);
+        cs[t][cs_at<D>(f)] = make_float2(fmaf(-sf, rest, cf), fmaf(cf, rest, sf));
     }
     __syncthreads();
 
-    // q, and k and v of the 16- and 32-bit caches: items of two eight-channel chunks.  Halves
-    // paired: chunk i with chunk i + half / 8.  Neighbours paired, or not rotated: two in a row.
-    constexpr int kItems = D / 16;
-    const int nq = a.q ? a.c.q_heads : 0, nkv = KIND == MKV_INT4 ? 0 : a.c.kv_heads;
-    const int per_tok = (nq + 2 * nkv) * kItems;
-    for (int i = tid; i < TT * per_tok; i += kAppendThreads) {
-        const int t = i / per_tok, r = i - t * per_tok;
-        if (place[t].skip) continue;
-        const int h = r / kItems, it = r - h * kItems;
-        const bool is_v = h >= nq + nkv, is_k = !is_v && h >= nq;
-        if ((is_v || is_k) && !place[t].page) continue;
-        const size_t tok = (size_t)(tok0 + t);
-        const T* src = is_v   ? (const T*)a.v + tok * a.v_stride + (size_t)(h - nq - nkv) * D
-                       : is_k ? (const T*)a.k + tok * a.k_stride + (size_t)(h - nq) * D
-                              : (const T*)a.q + tok * a.q_stride + (size_t)h * D;
-        uint8_t* dst8 = is_v   ? place[t].page + a.c.kv_bytes + (size_t)(h - nq - nkv) * a.c.head_bytes
-                        : is_k ? place[t].page + (size_t)(h - nq) * a.c.head_bytes
-                               : (uint8_t*)a.q_out + (tok * a.c.q_heads + h) * (size_t)D * sizeof(T);
-        T* dst = (T*)dst8 + ((is_v || is_k) ? (size_t)place[t].row * D : 0);
-        const bool turn = !is_v && it * 16 < a.rot_dim;
-        int c0 = 16 * it, c1 = 16 * it + 8;
-        if (turn && !a.interleaved) { c0 = 8 * it; c1 = 8 * it + half; }
-        float x[8], y[8];
-        Vec8<T>::load(src + c0, x);
-        Vec8<T>::load(src + c1, y);
-        if (turn) {
-            const float2* w = cs[t] + 8 * it;
-            if (a.interleaved) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 u = w[e], z = w[4 + e];
-                    const float x0 = x[2 * e], x1 = x[2 * e + 1], y0 = y[2 * e], y1 = y[2 * e + 1];
-                    x[2 * e] = x0 * u.x - x1 * u.y; x[2 * e + 1] = x1 * u.x + x0 * u.y;
-                    y[2 * e] = y0 * z.x - y1 * z.y; y[2 * e + 1] = y1 * z.x + y0 * z.y;
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float2 u = w[e];
-                    const float x0 = x[e], y0 = y[e];
-                    x[e] = x0 * u.x - y0 * u.y; y[e] = y0 * u.x + x0 * u.y;
-                }
-            }
-        }
-        Vec8<T>::store(dst + c0, x);
-        Vec8<T>::store(dst + c1, y);
-    }
-
-    if (KIND == MKV_INT4) {
-        // a lane owns four channels of one head and token; D / 4 lanes make a head
-        constexpr int kLanes = D / 4, NG = D / 32;
-        const int per4 = 2 * a.c.kv_heads * kLanes;
-        const int l = tid % kLanes;
-        const int total = TT * per4;   // a multiple of 32: whole warps stay together in the shuffles
-        for (int i = tid; i < (total + 31) / 32 * 32; i += kAppendThreads) {
-            const int t = min(i / per4, TT - 1), r = i - t * per4;
-            const int h = min(r / kLanes, 2 * a.c.kv_heads - 1);
-            const bool is_v = h >= a.c.kv_heads, live = i < total && !place[t].skip && place[t].page;
-            const int hk = is_v ? h - a.c.kv_heads : h;
-            double x[4] = {0, 0, 0, 0};
-            if (live) {
+    // q, and k and v of the 16- and 32-bit caches.  A thread has the same item of every head it takes: two chunks of eight
+    // channels.  Halves paired: chunk i with chunk i + half / 8.  Neighbours paired, or not rotated: two in a row.
+    constexpr int kItems = D / 16, kAtOnce = kAppendThreads / kItems;
+    const int nq = a.q && (KIND != MKV_INT4 || blockIdx.y == 1) ? a.c.q_heads : 0, nkv = KIND == MKV_INT4 ? 0 : a.c.kv_heads;
+    const int it = tid % kItems;
+    const bool rotated = it * 16 < a.rot_dim, split = rotated && !a.interleaved;
+    const int c0 = split ? 8 * it : 16 * it, c1 = split ? 8 * it + half : 16 * it + 8;
+    const int heads = nq + 2 * nkv;
+    if (heads > 0) {
+        // tokens and heads in one sequence, so that a thread's loads do not wait for one another's tokens
+#pragma unroll 2
+        for (int i = tid / kItems; i < TT * heads; i += kAtOnce) {
+            const int t = TT == 1 ? 0 : i / heads, h = i - t * heads;
+            const bool is_v = h >= nq + nkv, is_k = !is_v && h >= nq;
+            uint8_t* const page = place[t].page;
+            if (place[t].skip || ((is_v || is_k) && !page)) continue;
+            {
                 const size_t tok = (size_t)(tok0 + t);
-                const T* src = is_v ? (const T*)a.v + tok * a.v_stride + (size_t)hk * D
-                                    : (const T*)a.k + tok * a.k_stride + (size_t)hk * D;
-                const int c = 4 * l;
+                const int hk = is_v ? h - nq - nkv : h - nq, row = place[t].row;
+                const T* src = is_v   ? (const T*)a.v + tok * a.v_stride + (size_t)hk * D
+                               : is_k ? (const T*)a.k + tok * a.k_stride + (size_t)hk * D
+                                      : (const T*)a.q + tok * a.q_stride + (size_t)h * D;
+                T* dst = is_v   ? (T*)(page + a.c.kv_bytes + (size_t)hk * a.c.head_bytes) + row * D
+                         : is_k ? (T*)(page + (size_t)hk * a.c.head_bytes) + row * D
+                                : (T*)a.q_out + (tok * a.c.q_heads + h) * D;
+                float x[8], y[8];
+                Vec8<T>::load(src + c0, x);
+                Vec8<T>::load(src + c1, y);
+                if (rotated && !is_v) {
+                    float2 w[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = (double)(float)src[c + e];
-                if (!is_v && c < a.rot_dim) {
+                    for (int k = 0; k < 4; ++k) {
+                        const float4 z = *reinterpret_cast<const float4*>(&cs[t][k * (D / 8) + it * 2]);
+                        w[2 * k] = make_float2(z.x, z.y);
+                        w[2 * k + 1] = make_float2(z.z, z.w);
+                    }
                     if (a.interleaved) {
 #pragma unroll
-                        for (int e = 0; e < 4; e += 2) {
-                            const double2 w = csd[t][(c + e) >> 1];
-                            const double x0 = x[e], x1 = x[e + 1];
-                            x[e] = x0 * w.x - x1 * w.y; x[e + 1] = x1 * w.x + x0 * w.y;
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 u = w[e], z = w[4 + e];
+                            const float x0 = x[2 * e], x1 = x[2 * e + 1], y0 = y[2 * e], y1 = y[2 * e + 1];
+                            x[2 * e] = x0 * u.x - x1 * u.y; x[2 * e + 1] = x1 * u.x + x0 * u.y;
+                            y[2 * e] = y0 * z.x - y1 * z.y; y[2 * e + 1] = y1 * z.x + y0 * z.y;
                         }
                     } else {
-                        const bool up = c >= half;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const double2 w = csd[t][up ? c + e - half : c + e];
-                            const double o = (double)(float)src[up ? c + e - half : c + e + half];
-                            x[e] = up ? x[e] * w.x + o * w.y : x[e] * w.x - o * w.y;
+                        for (int e = 0; e < 8; ++e) {
+                            const float2 u = w[e];
+                            const float x0 = x[e], y0 = y[e];
+                            x[e] = x0 * u.x - y0 * u.y; y[e] = y0 * u.x + x0 * u.y;
                         }
                     }
                 }
+                Vec8<T>::store(dst + c0, x);
+                Vec8<T>::store(dst + c1, y);
             }
-            const Coded z = quantise4(x);
-            if (!live) continue;
-            uint8_t* blk = place[t].page + (size_t)hk * a.c.head_bytes + (size_t)(place[t].row >> 4) * paged_block_bytes(D);
-            const int row = place[t].row & 15, j = l >> 3, g = l & 7;
-            uint8_t* codes = is_v ? blk + 8 * D + (row >> 1) * D + (g * NG + j) * 4 + (row & 1) * 2
-                                  : blk + row * (D / 2) + ((g >> 1) * NG + j) * 4 + (g & 1) * 2;
-            *reinterpret_cast<uint16_t*>(codes) = (uint16_t)z.codes16;
-            if (g == 0) {
-                uint8_t* par = blk + 16 * D + (is_v ? 64 * NG : 0);
-                const int by_pair = ((row >> 1) * NG + j) * 4 + (row & 1) * 2;
-                *reinterpret_cast<uint16_t*>(par + by_pair) = z.scale;
-                *reinterpret_cast<uint16_t*>(par + 32 * NG + (is_v ? by_pair : (row * NG + j) * 2)) = z.lowest;
+        }
+    }
+
+    if (KIND == MKV_INT4 && blockIdx.y == 0) {
+        // A warp takes the same heads of two tokens whose rows share a pair (or of one token, where the other is not
+        // here).  A lane owns eight channels of both, D / 8 lanes make a head: one word of K for each token, two words of
+        // V that hold both.
+        constexpr int kLanes = D / 8, NG = D / 32, kHeads = 32 / kLanes, kTok = TT == 1 ? 1 : 2;
+        const int lane = tid & 31, l = lane % kLanes, j = l >> 2, g = l & 3, c = 8 * l;
+        const int hk2 = 2 * a.c.kv_heads;
+        const bool up = c >= half;
+        const int other = up ? c - half : c + half;
+        const int pair0 = a.interleaved ? c >> 1 : up ? c - half : c;
+        for (int h0 = (tid >> 5) * kHeads; h0 < hk2; h0 += kAppendThreads / 32 * kHeads) {
+            const int h = h0 + lane / kLanes;
+            const bool in = h < hk2, is_v = in && h >= a.c.kv_heads;
+            const int hk = !in ? 0 : is_v ? h - a.c.kv_heads : h;
+            const bool turn = !is_v && c < a.rot_dim, swap = turn && !a.interleaved;
+            const long long stride = is_v ? a.v_stride : a.k_stride;
+            const T* const head = (const T*)(is_v ? a.v : a.k) + (size_t)tok0 * stride + (size_t)hk * D;
+            const size_t out = (size_t)hk * a.c.head_bytes;
+            // this lane's words within a block (of row 0), and its parameters
+            const int word = is_v ? 8 * D + (2 * g * NG + j) * 4 : (g * NG + j) * 4, par = 16 * D + (is_v ? 64 * NG : 0) + j * 4;
+#pragma unroll 1
+            for (int t0 = 0; t0 < TT; ++t0) {
+                const int role = TT == 1 ? 1 : pairs[t0];
+                const TokenPlace at = place[t0];
+                if (role == 0 || at.skip || !at.page) continue;
+                const T* const src = head + t0 * stride;
+                float xs[kTok][8], os[kTok][8];
+#pragma unroll
+                for (int k = 0; k < kTok; ++k) {   // all loads on their way first
+                    const T* p = src + (role == 2 ? k * stride : 0);
+                    Vec8<T>::load(p + c, xs[k]);
+                    if (swap) Vec8<T>::load(p + other, os[k]);
+                }
+                Coded z[2];
+#pragma unroll
+                for (int k = 0; k < kTok; ++k) {
+                    if (k == 1 && role != 2) break;
+                    const float (&x)[8] = xs[k];
+                    const float (&o)[8] = os[k];
+                    float y[8], err[8];
+                    if (turn) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float2 f = cs[t0 + k][cs_at<D>(pair0 + (a.interleaved ? e >> 1 : e))];
+                            const float p = a.interleaved ? x[e ^ 1] : o[e];
+                            const bool second = a.interleaved ? (e & 1) : up;
+                            const float ps = p * f.y;
+                            y[e] = fmaf(x[e], f.x, second ? ps : -ps);
+                            err[e] = (fabsf(x[e]) + fabsf(p)) * 4.8e-7f;   // cos and sin 2^-22 off, the product and the sum rounded: 2^-21
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) { y[e] = x[e]; err[e] = 0.f; }
+                    }
+                    bool unsure;
+                    z[k] = quantise8(y, err, sizeof(T) == 2 && !turn, &unsure);
+                    if (__any_sync(0xffffffffu, unsure)) {
+                        const Coded wide = code_wide<T>(src + k * stride, c, turn, place[t0 + k].rot_pos, a.inv_freq, half, a.interleaved);
+                        if (z[k].scale != 0x7fc0) z[k] = wide;
+                    }
+                }
+                if (!in) continue;
+                uint8_t* const blk = at.page + out + (size_t)(at.row >> 4) * paged_block_bytes(D);
+                const int row = at.row & 15;
+                uint8_t* const w0 = blk + word + (is_v ? (row >> 1) * D : row * (D / 2));
+                uint8_t* const p0 = blk + par + (row >> 1) * (NG * 4);
+                uint16_t* const k_low = reinterpret_cast<uint16_t*>(blk + 16 * D + 32 * NG) + row * NG + j;
+                if (TT > 1 && role == 2) {
+                    if (is_v) {
+                        *reinterpret_cast<uint32_t*>(w0) = (z[0].codes & 0xffffu) | z[1].codes << 16;
+                        *reinterpret_cast<uint32_t*>(w0 + NG * 4) = z[0].codes >> 16 | (z[1].codes & 0xffff0000u);
+                    } else {
+                        *reinterpret_cast<uint32_t*>(w0) = z[0].codes;
+                        *reinterpret_cast<uint32_t*>(w0 + D / 2) = z[1].codes;
+                    }
+                    if (g == 0) {
+                        *reinterpret_cast<uint32_t*>(p0) = z[0].scale | (uint32_t)z[1].scale << 16;
+                        if (is_v) {
+                            *reinterpret_cast<uint32_t*>(p0 + 32 * NG) = z[0].lowest | (uint32_t)z[1].lowest << 16;
+                        } else {
+                            k_low[0] = z[0].lowest;
+                            k_low[NG] = z[1].lowest;
+                        }
+                    }
+                } else {
+                    const int odd = (row & 1) * 2;
+                    if (is_v) {
+                        *reinterpret_cast<uint16_t*>(w0 + odd) = (uint16_t)z[0].codes;
+                        *reinterpret_cast<uint16_t*>(w0 + NG * 4 + odd) = (uint16_t)(z[0].codes >> 16);
+                    } else {
+                        *reinterpret_cast<uint32_t*>(w0) = z[0].codes;
+                    }
+                    if (g == 0) {
+                        *reinterpret_cast<uint16_t*>(p0 + odd) = z[0].scale;
+                        if (is_v) *reinterpret_cast<uint16_t*>(p0 + 32 * NG + odd) = z[0].lowest;
+                        else k_low[0] = z[0].lowest;
+                    }
+                }
             }
         }
     }
@@ -296,8 +434,9 @@ __global__ void __launch_bounds__(kAppendThreads) paged_read_kernel(const PagedR
 template <typename T, int KIND, int D>
 cudaError_t append_t(const PagedAppendArgs& a, cudaStream_t st) {
     constexpr int TT = 4;
-    if (a.b.n_tokens <= 1024) paged_append_kernel<T, KIND, D, 1><<<a.b.n_tokens, kAppendThreads, 0, st>>>(a);
-    else paged_append_kernel<T, KIND, D, TT><<<(a.b.n_tokens + TT - 1) / TT, kAppendThreads, 0, st>>>(a);
+    const unsigned y = KIND == MKV_INT4 && a.q ? 2 : 1;
+    if (a.b.n_tokens <= 1024) paged_append_kernel<T, KIND, D, 1><<<dim3(a.b.n_tokens, y), kAppendThreads, 0, st>>>(a);
+    else paged_append_kernel<T, KIND, D, TT><<<dim3((a.b.n_tokens + TT - 1) / TT, y), kAppendThreads, 0, st>>>(a);
     return cudaGetLastError();
 }
 template <typename T, int KIND, int D>
