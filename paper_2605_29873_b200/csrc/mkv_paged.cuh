@@ -29,8 +29,9 @@ namespace mkv {
 
 constexpr int kPagedBlock = 16;     // tokens of a 4-bit block; also the granule of the attention kernels
 constexpr int kPagedMaxGroup = 32;  // q_heads / kv_heads
-constexpr int kPagedTickets = 1024;  // most CTAs of a launch that joins parts of units
-constexpr int kPagedTileCtas = 160;  // most CTAs of a launch of the kernel for many rows
+constexpr int kPagedDecodeCtas = 512;   // most CTAs of a launch of the kernel for few rows
+constexpr int kPagedJoinBytes = 65536;  // of the workspace, in front of the parts
+constexpr int kPagedTileCtas = 160;    // most CTAs of a launch of the kernel for many rows
 constexpr float kPagedNegInf = -INFINITY;
 
 struct PagedDev {
@@ -120,13 +121,13 @@ __device__ inline float paged_bf16(uint32_t bits16) { return __uint_as_float(bit
 
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int head_dim, cudaStream_t st);
 cudaError_t launch_paged_read(const PagedReadArgs& a, int head_dim, cudaStream_t st);
-size_t paged_decode_scratch();   // workspace of launch_paged_decode, zero before its first launch
+size_t paged_decode_scratch();   // workspace of launch_paged_decode
 bool make_paged_map(void* map, const void* pages, long long rows, int head_dim, int box_rows);   // bf16 pages as one list of rows
 cudaError_t launch_paged_decode(const PagedAttendArgs& a, int head_dim, const void* map, long long layer_rows, int sm_count,
-                                cudaStream_t st);
+                                int device, cudaStream_t st);
 
 size_t paged_tile_scratch();
 cudaError_t launch_paged_tile(const PagedAttendArgs& a, int head_dim, const void* map, long long layer_rows, int sm_count,
-                              cudaStream_t st);
+                              int device, cudaStream_t st);
 
 }  // namespace mkv

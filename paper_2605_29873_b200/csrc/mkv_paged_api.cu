@@ -39,12 +39,12 @@ bool shape_ok(int kv_heads, int head_dim, int page_size, int kv_dtype) {
 }
 
 struct DeviceGuard {
-    int prev = -1; bool ok;
-    explicit DeviceGuard(int dev) {
+    int prev = -1; const int dev; bool ok;
+    explicit DeviceGuard(int device) : dev(device) {
         ok = cudaGetDevice(&prev) == cudaSuccess;
         if (ok && prev != dev) ok = cudaSetDevice(dev) == cudaSuccess;
     }
-    ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
+    ~DeviceGuard() { if (prev >= 0 && prev != dev) cudaSetDevice(prev); }
 };
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
@@ -135,7 +135,7 @@ mkv_status mkv_paged_create(int layers, int q_heads, int kv_heads, int head_dim,
         delete c;
         return MKV_ERR_CUDA;
     }
-    if (cudaMemset(workspace, 0, paged_ws().total) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+    if (cudaMemset(workspace, 0, paged_ws().scratch) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
         delete c;
         return MKV_ERR_CUDA;
     }
@@ -206,10 +206,10 @@ mkv_status mkv_paged_attend(mkv_paged* c, int layer, const void* q, int64_t q_st
     // Few rows of a sequence and head: the cache is streamed, a unit's rows on one pass.  Many: tiles on the tensor
     // cores.  fp32 pages have the first form only.
     const cudaError_t e = c->kv_dtype == MKV_F32 || (long long)a.c.group * a.max_new <= 64
-                              ? launch_paged_decode(a, c->head_dim, &c->map16, layer * rows_per_layer, c->sm_count, st)
-                              : launch_paged_tile(a, c->head_dim, &c->map_page, layer * rows_per_layer, c->sm_count, st);
+                              ? launch_paged_decode(a, c->head_dim, &c->map16, layer * rows_per_layer, c->sm_count, c->device, st)
+                              : launch_paged_tile(a, c->head_dim, &c->map_page, layer * rows_per_layer, c->sm_count, c->device, st);
     if (e != cudaSuccess) return MKV_ERR_CUDA;
-    c->launches += 1;
+    c->launches += 2;
     return MKV_OK;
 }
 
@@ -246,7 +246,6 @@ mkv_status mkv_paged_reset(mkv_paged* c) {
     if (!guard.ok || cudaDeviceSynchronize() != cudaSuccess) return MKV_ERR_CUDA;
     const PagedWs w = paged_ws();
     if (cudaMemset(c->ws + w.status, 0, 4) != cudaSuccess) return MKV_ERR_CUDA;
-    if (w.total > w.scratch && cudaMemset(c->ws + w.scratch, 0, w.total - w.scratch) != cudaSuccess) return MKV_ERR_CUDA;
     return MKV_OK;
 }
 

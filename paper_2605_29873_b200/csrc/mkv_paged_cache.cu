@@ -3,7 +3,7 @@
 // three dependent loads (starts, lens, table) for single tokens.
 #include <cfloat>
 
-#include "mkv_paged.cuh"
+#include "mkv_paged_units.cuh"
 
 namespace mkv {
 namespace {
@@ -196,6 +196,8 @@ __global__ void __launch_bounds__(kAppendThreads, KIND == MKV_INT4 ? 3 : 5) page
     __shared__ int pairs[TT];
     __shared__ __align__(16) float2 cs[TT][D / 2];
     const int tid = threadIdx.x, tok0 = blockIdx.x * TT;
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
     if (tid < TT && tok0 + tid < a.b.n_tokens) place[tid] = token_place(a, tok0 + tid);
     else if (tid < TT) place[tid].skip = 1;
     __syncthreads();
@@ -386,6 +388,8 @@ __global__ void __launch_bounds__(kAppendThreads, KIND == MKV_INT4 ? 3 : 5) page
 template <typename T, int KIND, int D>
 __global__ void __launch_bounds__(kAppendThreads) paged_read_kernel(const PagedReadArgs a) {
     const int s = blockIdx.y, h = blockIdx.z;
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
     const PagedSpan sp = paged_span(a.c, a.b, s);
     int first = a.first ? a.first[s] : 0;
     if (first < 0) { paged_fail(a.c, MKV_ERR_INVALID_ARG); first = 0; }
@@ -435,16 +439,14 @@ template <typename T, int KIND, int D>
 cudaError_t append_t(const PagedAppendArgs& a, cudaStream_t st) {
     constexpr int TT = 4;
     const unsigned y = KIND == MKV_INT4 && a.q ? 2 : 1;
-    if (a.b.n_tokens <= 1024) paged_append_kernel<T, KIND, D, 1><<<dim3(a.b.n_tokens, y), kAppendThreads, 0, st>>>(a);
-    else paged_append_kernel<T, KIND, D, TT><<<dim3((a.b.n_tokens + TT - 1) / TT, y), kAppendThreads, 0, st>>>(a);
-    return cudaGetLastError();
+    if (a.b.n_tokens <= 1024) return paged_launch(paged_append_kernel<T, KIND, D, 1>, dim3(a.b.n_tokens, y), kAppendThreads, 0, st, a);
+    return paged_launch(paged_append_kernel<T, KIND, D, TT>, dim3((a.b.n_tokens + TT - 1) / TT, y), kAppendThreads, 0, st, a);
 }
 template <typename T, int KIND, int D>
 cudaError_t read_t(const PagedReadArgs& a, cudaStream_t st) {
     const int per = kAppendThreads / (D / 8);
     const dim3 grid((unsigned)min((a.rows + per - 1) / per, 64), (unsigned)a.b.batch, (unsigned)a.c.kv_heads);
-    paged_read_kernel<T, KIND, D><<<grid, kAppendThreads, 0, st>>>(a);
-    return cudaGetLastError();
+    return paged_launch(paged_read_kernel<T, KIND, D>, grid, kAppendThreads, 0, st, a);
 }
 
 }  // namespace

@@ -4,8 +4,7 @@
 // Work.  A unit is one (sequence, KV head, tile of RT rows); its cache rows are blocks of 16 tokens.
 // All units' blocks form one list (sequence, head, row tile, block), cut into one contiguous range
 // per CTA, so CTAs get equal shares whatever the lengths, and the cut depends on nothing but the
-// lengths: the same inputs give the same bits.  Lengths are on the device; every CTA sums them for
-// itself.  The warps of a CTA take the blocks of a unit in turn, each with its own online softmax
+// lengths.  The warps of a CTA take the blocks of a unit in turn, each with its own online softmax
 // (m, l, O) and its own ring of shared-memory stages that its lane 0 fills by bulk copies, several
 // blocks ahead and across unit borders; nothing but the end of a unit makes the warps meet.  There
 // they add up their states.  A unit cut by range borders leaves its parts in the workspace, and the
@@ -63,11 +62,7 @@ struct Cfg {
     static constexpr int kSmem = 1024 + kRing + kMerge + kMl + kWeights;
 };
 
-__device__ inline float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
+__device__ inline float ex2(float x) { return paged_ex2(x); }
 __device__ inline void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -98,31 +93,6 @@ __device__ inline void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
         ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
-
-struct Part { float *o, *m, *l; };
-// Part `slot` of the workspace: O [RT][D], m [RT], l [RT]
-template <int RT, int D>
-__device__ inline Part part_at(const PagedAttendArgs& a, int slot) {
-    float* p = reinterpret_cast<float*>(a.scratch + kPagedTickets * 4) + (size_t)slot * RT * (D + 2);
-    return {p, p + RT * D, p + RT * D + RT};
-}
-
-template <int D>
-__device__ inline void store_row(const PagedAttendArgs& a, const Unit& u, int row, int c, float4 o, float m, float l) {
-    const int r = u.row0 + row, j = r / a.c.group, h = u.h * a.c.group + (r - j * a.c.group);
-    const size_t at = (size_t)(u.tok0 + j) * a.c.q_heads + h;
-    // l is 0 where nothing was seen and NaN where a NaN was
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (a.c.out_f32) {
-        *reinterpret_cast<float4*>((float*)a.out + at * D + c) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    } else {
-        uint2 w;
-        w.x = ptx::pack_bf16x2(o.x * inv, o.y * inv);
-        w.y = ptx::pack_bf16x2(o.z * inv, o.w * inv);
-        *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + at * D + c) = w;
-    }
-    if (a.lse && c == 0) a.lse[at] = l == 0.f ? kPagedNegInf : (m + log2f(l)) * 0.69314718055994531f;
 }
 
 // A warp's state over the blocks it has worked through.
@@ -692,6 +662,12 @@ __device__ inline void put_state(State<D, NT>& st, float* o, float2* ml, int lan
     }
 }
 
+// A block for every warp at least, and no more ranges in a unit than its join can read quickly.
+struct DecodeRanges {
+    long long units;
+    __device__ long long operator()(long long total) const { return min(total / kW, units * kMaxParts); }
+};
+
 template <int D, int NT>
 __device__ inline void clear(State<D, NT>& st) {
 #pragma unroll
@@ -716,14 +692,12 @@ __device__ inline void clear(StateF32<D>& st) {
 
 template <int KIND, int D, int NT, bool Q32, bool HL>
 __global__ void __launch_bounds__(kThreads, KIND == MKV_INT4 && NT == 1 ? 2 : 1)
-paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendArgs a, long long layer_rows) {
+paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendArgs a, long long layer_rows, DecodeRanges want) {
     using C = Cfg<KIND, D, NT>;
     constexpr int RT = C::RT, DP = C::DP;
     extern __shared__ uint8_t raw_smem[];
     __shared__ __align__(8) unsigned long long bars[kW * C::kStages];
-    __shared__ Unit s_unit;
-    __shared__ long long s_scan[kW];
-    __shared__ int s_last;
+    __shared__ FindShared fs;
     uint8_t* const smem = raw_smem + ((1024u - (ptx::smem_u32(raw_smem) & 1023u)) & 1023u);
     float* const merge = reinterpret_cast<float*>(smem + C::kRing);
     float2* const mls = reinterpret_cast<float2*>(smem + C::kRing + C::kMerge);
@@ -733,19 +707,17 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
         for (int i = 0; i < kW * C::kStages; ++i) ptx::mbar_init(ptx::smem_u32(&bars[i]), 1);
         ptx::fence_barrier_init();
     }
-    // a block for every warp at least, and no more ranges in a unit than its end can join quickly
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
     Range rg;
-    if (!find_range<RT, 16, kThreads>(a, rg, &s_unit, s_scan, [&](long long total) {
-            const long long units = (long long)a.b.batch * a.c.kv_heads;
-            return min(total / kW, units * kMaxParts);
-        }))
-        return;
+    Unit f;
+    if (!find_unit<RT, 16, kThreads>(a, rg, f, fs, want)) return;
     const long long t0 = rg.t0, t1 = rg.t1;
+    __syncthreads();   // the barriers are ready
 
     // ---- this warp's fetches: unit f, blocks f_lo + warp, + kW, ... of its part [f_lo, f_hi) in the range
     const uint32_t ring = ptx::smem_u32(smem) + warp * C::kStages * C::kStage;
     const uint32_t bar0 = ptx::smem_u32(&bars[warp * C::kStages]);
-    Unit f = s_unit;
     Unit u = f;
     bool more = true;
     int f_i = warp, f_n, f_first, page_of = 0, f_stage = 0, in_flight = 0;
@@ -846,7 +818,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
         __syncthreads();
         // ---- the warps' states become one
         const bool whole = lo == u.base && hi == u.end();
-        const Part part = part_at<RT, D>(a, 2 * blockIdx.x + (t0 < u.base ? 1 : 0));
+        const PartOf<RT, D, false> part(a, 2 * blockIdx.x + (t0 < u.base ? 1 : 0));
         for (int i = tid; i < RT * (D / 4); i += kThreads) {
             const int row = i / (D / 4), c = (i - row * (D / 4)) * 4;
             float m = -FLT_MAX, l = 0.f;
@@ -862,47 +834,17 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
                 o.x = fmaf(y.x, f2, o.x); o.y = fmaf(y.y, f2, o.y); o.z = fmaf(y.z, f2, o.z); o.w = fmaf(y.w, f2, o.w);
             }
             if (whole) {
-                if (row < u.rows) store_row<D>(a, u, row, c, o, m, l);
+                if (row < u.rows) store4<D>(a, u, row, c, o, m, l);
             } else {
-                *reinterpret_cast<float4*>(part.o + row * D + c) = o;
-                if (c == 0) { part.m[row] = m; part.l[row] = l; }
+                *part.at(row, c / 4) = o;
+                if (c == 0) { *part.m(row) = m; *part.l(row) = l; }
             }
         }
-        if (!whole) {
-            // the ranges that this unit spans: first and last
-            const int c0 = rg.of(u.base), c1 = rg.of(u.end() - 1);
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                int* ticket = reinterpret_cast<int*>(a.scratch) + c0;
-                s_last = atomicAdd(ticket, 1) == c1 - c0;
-                if (s_last) *ticket = 0;   // for the next launch
-                __threadfence();
-            }
-            __syncthreads();
-            if (s_last) {
-                for (int i = tid; i < u.rows * (D / 4); i += kThreads) {
-                    const int row = i / (D / 4), c = (i - row * (D / 4)) * 4;
-                    float m = -FLT_MAX, l = 0.f;
-                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                    const int first_slot = 2 * c0 + (rg.begin_of(c0) < u.base ? 1 : 0);
-                    for (int r = c0; r <= c1; ++r) {
-                        const Part p = part_at<RT, D>(a, r == c0 ? first_slot : 2 * r);
-                        const float pm = __ldcg(p.m + row), pl = __ldcg(p.l + row);
-                        const float4 y = __ldcg(reinterpret_cast<const float4*>(p.o + row * D + c));
-                        const float mn = fmaxf(m, pm), f1 = ex2(m - mn), f2 = ex2(pm - mn);
-                        l = fmaf(pl, f2, l * f1);
-                        o.x = fmaf(y.x, f2, o.x * f1); o.y = fmaf(y.y, f2, o.y * f1);
-                        o.z = fmaf(y.z, f2, o.z * f1); o.w = fmaf(y.w, f2, o.w * f1);
-                        m = mn;
-                    }
-                    store_row<D>(a, u, row, c, o, m, l);
-                }
-            }
-        }
-        if (u.end() >= t1 || !next_unit<RT, 16>(a, u)) break;
+        if (u.end() >= t1) break;
+        next_unit<RT, 16>(a, u);
         __syncthreads();   // the merge buffer is free again
     }
+    if (tid == 0) leave_join(a, rg, u);
     // copies still on their way after a wait that ran out
     while (in_flight > 0) {
         paged_wait(bar0 + stage * 8, parity);
@@ -912,19 +854,22 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
 }
 
 template <int KIND, int D, int NT, bool Q32, bool HL>
-cudaError_t decode_t(const PagedAttendArgs& a, const CUtensorMap& map, long long layer_rows, int sm_count, cudaStream_t st) {
+cudaError_t decode_t(const PagedAttendArgs& a, const CUtensorMap& map, long long layer_rows, int sm_count, int device, cudaStream_t st) {
     using C = Cfg<KIND, D, NT>;
+    static std::atomic<unsigned long long> ready;
     auto* fn = paged_decode_kernel<KIND, D, NT, Q32, HL>;
-    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+    cudaError_t e = paged_opt_in(ready, fn, C::kSmem, device);
     if (e != cudaSuccess) return e;
-    const int grid = min(sm_count * (KIND == MKV_INT4 && NT == 1 ? 2 : 1), kPagedTickets);
-    fn<<<grid, kThreads, C::kSmem, st>>>(map, a, layer_rows);
-    return cudaGetLastError();
+    const int grid = min(sm_count * (KIND == MKV_INT4 && NT == 1 ? 2 : 1), kPagedDecodeCtas);
+    const DecodeRanges want{(long long)a.b.batch * a.c.kv_heads};
+    e = paged_launch(fn, dim3(grid), kThreads, C::kSmem, st, map, a, layer_rows, want);
+    if (e != cudaSuccess) return e;
+    return paged_launch(paged_join_kernel<C::RT, D, false, 4, 1>, dim3(grid, (C::RT * D + 1023) / 1024), 1024, 0, st, a);
 }
 
 }  // namespace
 
-size_t paged_decode_scratch() { return kPagedTickets * 4 + (size_t)2 * kPagedTickets * 16 * (128 + 2) * 4; }
+size_t paged_decode_scratch() { return kPagedJoinBytes + (size_t)2 * kPagedDecodeCtas * 16 * (128 + 2) * 4; }
 
 bool make_paged_map(void* map, const void* pages, long long rows, int head_dim, int box_rows) {
     using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -942,12 +887,13 @@ bool make_paged_map(void* map, const void* pages, long long rows, int head_dim, 
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-cudaError_t launch_paged_decode(const PagedAttendArgs& a, int D, const void* map, long long layer_rows, int sm_count, cudaStream_t st) {
+cudaError_t launch_paged_decode(const PagedAttendArgs& a, int D, const void* map, long long layer_rows, int sm_count, int device,
+                                cudaStream_t st) {
     const CUtensorMap& m = *(const CUtensorMap*)map;
     const bool one = (long long)a.c.group * a.max_new <= 8;
 #define MKV_GO(KIND, NT, Q32, HL)                                                                  \
-    return D == 128 ? decode_t<KIND, 128, NT, Q32, HL>(a, m, layer_rows, sm_count, st)             \
-                    : decode_t<KIND, 64, NT, Q32, HL>(a, m, layer_rows, sm_count, st)
+    return D == 128 ? decode_t<KIND, 128, NT, Q32, HL>(a, m, layer_rows, sm_count, device, st)             \
+                    : decode_t<KIND, 64, NT, Q32, HL>(a, m, layer_rows, sm_count, device, st)
     if (a.c.kv_dtype == MKV_F32) { MKV_GO(MKV_F32, 1, false, false); }
     if (a.c.kv_dtype == MKV_BF16) {
         if (one) { MKV_GO(MKV_BF16, 1, false, false); }

@@ -103,11 +103,7 @@ __host__ __device__ constexpr uint32_t mma_desc(int type, int n, bool b_outer) {
     return 1u << 4 | (uint32_t)type << 7 | (uint32_t)type << 10 | (uint32_t)b_outer << 16 | (uint32_t)(n >> 3) << 17 | (128u >> 4) << 24;
 }
 
-__device__ inline float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
+__device__ inline float ex2(float x) { return paged_ex2(x); }
 __device__ inline uint32_t pack_f16x2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -137,13 +133,12 @@ struct Shared {
     unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2];
     uint32_t tmem;
     int dead;                       // a wait ran out: everybody leaves
-    int last;
     int n_odd;
     int2 odd[kOddMax];              // (tile of this CTA, position), a ring
     float k_mul[2], v_exp[2];       // 4 bits: what the stage's K and V were divided by (a factor, a log2)
     float red[8];
-    long long scan[16];
-    Unit unit;
+    FindShared find;
+    Unit unit;                      // the first of this CTA
 };
 
 // Waits that end: false once any of the CTA's waits ran out.
@@ -163,19 +158,6 @@ __device__ inline bool any_leaves(bool leave) {
         "barrier.cta.red.or.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
         : "=r"(r) : "r"((uint32_t)leave) : "memory");
     return r != 0;
-}
-__device__ inline void soft_barrier() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
-
-// A part of a unit in the workspace: four channels of all 256 rows, the next four, ... (a warp's rows next to one
-// another), then m and l.
-struct TilePart {
-    float *o, *m, *l;
-    __device__ float4* at(int row, int c) const { return reinterpret_cast<float4*>(o) + (c >> 2) * kRows + row; }
-};
-template <int D>
-__device__ inline TilePart tile_part(const PagedAttendArgs& a, int slot) {
-    float* p = reinterpret_cast<float*>(a.scratch + kPagedTickets * 4) + (size_t)slot * kRows * (D + 2);
-    return {p, p + kRows * D, p + kRows * D + kRows};
 }
 
 // position of row r (of the unit's) and where its output goes
@@ -496,11 +478,14 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
             o_par ^= 1;
             fence_after();
         }
-        if (any_leaves(!ok)) return;   // and the list of odd tokens is complete
+        if (any_leaves(!ok)) {   // and the list of odd tokens is complete
+            if (tid == 0) join_of(a, blockIdx.x)->last = -1;
+            return;
+        }
         // ---- the row's result, or its part
         const bool whole = lo == u.base && hi == u.end();
         uint8_t* const out_row = live ? (uint8_t*)a.out + place.at * (D * (a.c.out_f32 ? 4 : 2)) : nullptr;
-        const TilePart part = tile_part<D>(a, 2 * blockIdx.x + (rg.t0 < u.base ? 1 : 0));
+        const PartOf<kRows, D, true> part(a, 2 * blockIdx.x + (rg.t0 < u.base ? 1 : 0));
         if (active) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
             const int n_odd = *(volatile int*)&sh.n_odd;
@@ -535,58 +520,19 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                     store32<D>(a, rows_out, out_row, 32 * c, o, inv);
                 } else if (live) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) *part.at(r, 32 * c + 4 * i) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    for (int i = 0; i < 8; ++i) *part.at(r, 8 * c + i) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                 }
             }
             fence_before();
             if (live && whole && a.lse) a.lse[place.at] = l == 0.f ? kPagedNegInf : (m + log2f(l)) * 0.69314718055994531f;
-            if (live && !whole) { part.m[r] = m; part.l[r] = l; }
+            if (live && !whole) { *part.m(r) = m; *part.l(r) = l; }
         }
         tiles += nt;
-        if (!whole) {
-            const int c0 = rg.of(u.base), c1 = rg.of(u.end() - 1);
-            __threadfence();
-            soft_barrier();
-            if (tid == 0) {
-                int* ticket = reinterpret_cast<int*>(a.scratch) + c0;
-                sh.last = atomicAdd(ticket, 1) == c1 - c0;
-                if (sh.last) *ticket = 0;   // for the next launch
-                __threadfence();
-            }
-            soft_barrier();
-            if (sh.last && active) {
-                const int slot0 = 2 * c0 + (rg.begin_of(c0) < u.base ? 1 : 0);
-                // two passes over the parts: the common reference, then the sums; four parts' loads on their way at a time
-                float mm = -FLT_MAX, ll = 0.f;
-                auto part_of = [&](int x) { return tile_part<D>(a, x == c0 ? slot0 : 2 * x); };
-#pragma unroll 4
-                for (int x = c0; x <= c1; ++x) mm = fmaxf(mm, __ldcg(part_of(x).m + r));
-#pragma unroll 4
-                for (int x = c0; x <= c1; ++x) ll = fmaf(__ldcg(part_of(x).l + r), ex2(__ldcg(part_of(x).m + r) - mm), ll);
-                const float inv = ll == 0.f ? 0.f : 1.f / ll;
-#pragma unroll 1
-                for (int c = 0; c < D / 32; ++c) {
-                    float o[32];
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = 0.f;
-#pragma unroll 2
-                    for (int x = c0; x <= c1; ++x) {
-                        const TilePart p = part_of(x);
-                        const float sc = ex2(__ldcg(p.m + r) - mm);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float4 z = __ldcg(p.at(r, 32 * c + 4 * i));
-                            o[4 * i] = fmaf(z.x, sc, o[4 * i]); o[4 * i + 1] = fmaf(z.y, sc, o[4 * i + 1]);
-                            o[4 * i + 2] = fmaf(z.z, sc, o[4 * i + 2]); o[4 * i + 3] = fmaf(z.w, sc, o[4 * i + 3]);
-                        }
-                    }
-                    store32<D>(a, rows_out, out_row, 32 * c, o, inv);
-                }
-                if (live && a.lse) a.lse[place.at] = ll == 0.f ? kPagedNegInf : (mm + log2f(ll)) * 0.69314718055994531f;
-            }
+        if (u.end() >= rg.t1) {
+            if (tid == 0) leave_join(a, rg, u);
+            return;
         }
-        if (u.end() >= rg.t1 || !next_unit<kRows, kTile>(a, u)) return;
-        soft_barrier();   // sh.last has been read
+        next_unit<kRows, kTile>(a, u);
     }
 }
 
@@ -869,17 +815,27 @@ __device__ inline void dequant_role(const PagedAttendArgs& a, Shared& sh, const 
     }
 }
 
+// Two tiles for a range at least, so that joining parts does not outweigh them.
+struct TileRanges {
+    __device__ long long operator()(long long total) const { return (total + 1) / 2; }
+};
+
 template <int KIND, int D, bool IO32>
 __global__ void __launch_bounds__(threads_of<KIND>(), 1)
-paged_tile_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendArgs a, long long layer_rows) {
+paged_tile_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendArgs a, long long layer_rows, TileRanges want) {
     using C = TileCfg<D>;
     extern __shared__ uint8_t raw_smem[];
     __shared__ Shared sh;
     const uint32_t smem = (ptx::smem_u32(raw_smem) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5;
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
     Range rg;
-    // a few tiles for a range, so that joining parts does not outweigh them
-    if (!find_range<kRows, kTile, threads_of<KIND>()>(a, rg, &sh.unit, sh.scan, [](long long total) { return (total + 1) / 2; })) return;
+    {
+        Unit u;
+        if (!find_unit<kRows, kTile, threads_of<KIND>()>(a, rg, u, sh.find, want)) return;
+        if (tid == 0) sh.unit = u;
+    }
     if (tid == 0) {
         auto init = [](unsigned long long& b, int n) { ptx::mbar_init(ptx::smem_u32(&b), n); };
         for (int i = 0; i < 2; ++i) {
@@ -911,25 +867,29 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendArgs
 }
 
 template <int KIND, int D, bool IO32>
-cudaError_t tile_t(const PagedAttendArgs& a, const CUtensorMap& map, long long layer_rows, int sm_count, cudaStream_t st) {
+cudaError_t tile_t(const PagedAttendArgs& a, const CUtensorMap& map, long long layer_rows, int sm_count, int device, cudaStream_t st) {
+    static std::atomic<unsigned long long> ready;
     auto* fn = paged_tile_kernel<KIND, D, IO32>;
-    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, TileCfg<D>::kSmem);
+    cudaError_t e = paged_opt_in(ready, fn, TileCfg<D>::kSmem, device);
     if (e != cudaSuccess) return e;
-    fn<<<min(sm_count, kPagedTileCtas), threads_of<KIND>(), TileCfg<D>::kSmem, st>>>(map, a, layer_rows);
-    return cudaGetLastError();
+    const int grid = min(sm_count, kPagedTileCtas);
+    e = paged_launch(fn, dim3(grid), threads_of<KIND>(), TileCfg<D>::kSmem, st, map, a, layer_rows, TileRanges());
+    if (e != cudaSuccess) return e;
+    return paged_launch(paged_join_kernel<kRows, D, true, 1, 4>, dim3(grid, kRows * D / 4096), 256, 0, st, a);
 }
 
 }  // namespace
 
-size_t paged_tile_scratch() { return kPagedTickets * 4 + (size_t)2 * kPagedTileCtas * kRows * (128 + 2) * 4; }
+size_t paged_tile_scratch() { return kPagedJoinBytes + (size_t)2 * kPagedTileCtas * kRows * (128 + 2) * 4; }
 
-cudaError_t launch_paged_tile(const PagedAttendArgs& a, int D, const void* map, long long layer_rows, int sm_count, cudaStream_t st) {
+cudaError_t launch_paged_tile(const PagedAttendArgs& a, int D, const void* map, long long layer_rows, int sm_count, int device,
+                              cudaStream_t st) {
     const CUtensorMap& m = *(const CUtensorMap*)map;
     if (a.c.kv_dtype == MKV_BF16)
-        return D == 128 ? tile_t<MKV_BF16, 128, false>(a, m, layer_rows, sm_count, st) : tile_t<MKV_BF16, 64, false>(a, m, layer_rows, sm_count, st);
+        return D == 128 ? tile_t<MKV_BF16, 128, false>(a, m, layer_rows, sm_count, device, st) : tile_t<MKV_BF16, 64, false>(a, m, layer_rows, sm_count, device, st);
     if (a.c.io_f32)
-        return D == 128 ? tile_t<MKV_INT4, 128, true>(a, m, layer_rows, sm_count, st) : tile_t<MKV_INT4, 64, true>(a, m, layer_rows, sm_count, st);
-    return D == 128 ? tile_t<MKV_INT4, 128, false>(a, m, layer_rows, sm_count, st) : tile_t<MKV_INT4, 64, false>(a, m, layer_rows, sm_count, st);
+        return D == 128 ? tile_t<MKV_INT4, 128, true>(a, m, layer_rows, sm_count, device, st) : tile_t<MKV_INT4, 64, true>(a, m, layer_rows, sm_count, device, st);
+    return D == 128 ? tile_t<MKV_INT4, 128, false>(a, m, layer_rows, sm_count, device, st) : tile_t<MKV_INT4, 64, false>(a, m, layer_rows, sm_count, device, st);
 }
 
 }  // namespace mkv

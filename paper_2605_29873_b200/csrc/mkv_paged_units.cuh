@@ -1,14 +1,21 @@
 // The work of an attention launch as one list: units (sequence, KV head, tile of RT rows) in order, each a
 // number of blocks of BLK cached tokens.  The list is cut into one contiguous range per CTA; lengths are on
-// the device, so every CTA sums them for itself.
+// the device, so every CTA sums them for itself.  A unit that lies in one range is finished by its CTA; of the
+// others every range leaves a part in the workspace, and a second launch joins the parts, in the order of the
+// ranges: the same inputs give the same bits.  (Joining in the launch itself, by the CTA that delivers the last
+// part, cost two to three round trips to memory at the end of every cut unit: 16.4 us where this takes TJOIN1 for
+// one sequence of 1025 tokens, 26 us against TJOIN2 for 4099 tokens of 4 bits.)
 #pragma once
+#include <atomic>
+#include <cfloat>
+
 #include "mkv_paged.cuh"
 #include "mkv_ptx.cuh"
 
 namespace mkv {
 
-// Bounded wait, for a few seconds at most.  The limit is counted in cycles: reading the global timer takes longer than
-// most waits do (the kernel for many rows ran KTIME with it).
+// Bounded wait, for a few seconds at most.  The limit is counted in cycles: reading the global timer takes longer
+// than most waits do.
 __device__ inline bool paged_wait(uint32_t bar, uint32_t parity) {
     for (int i = 0; i < 16; ++i)
         if (ptx::mbar_try_wait(bar, parity)) return true;
@@ -45,7 +52,7 @@ __device__ inline void unit_rows(const PagedAttendArgs& a, Unit& u) {
 }
 template <int RT> __device__ inline int row_tiles(const PagedAttendArgs& a, int n) { return (n * a.c.group + RT - 1) / RT; }
 
-// Blocks of one head of sequence s in the list.
+// Blocks of one head of a sequence in the list.
 template <int RT, int BLK>
 __device__ inline long long blocks_per_head(const PagedAttendArgs& a, const PagedSpan& sp) {
     Unit u;
@@ -75,24 +82,71 @@ __device__ inline bool next_unit(const PagedAttendArgs& a, Unit& u) {
     return true;
 }
 
-// Length of the list, and which range of it this CTA has.  Called by all threads of a block of THREADS; the
-// thread that finds the first unit leaves it in *first.  `want(total)`: the number of ranges.  Returns false
-// where the CTA has no work (for all threads alike).
+// The list as it is cut: n ranges of equal length.
 struct Range {
-    long long total, t0, t1;
-    int n;   // ranges
-    __device__ long long begin_of(int r) const { return total * r / n; }
+    long long total, t0, t1;   // this CTA's range [t0, t1)
+    int n;
+    __device__ long long begin_of(int r) const {
+        const unsigned long long x = (unsigned long long)total * (unsigned)r;
+        return x >> 32 ? (long long)(x / (unsigned)n) : (long long)((unsigned)x / (unsigned)n);
+    }
     __device__ int of(long long t) const {
-        int r = (int)(t * n / total);
+        const unsigned long long x = (unsigned long long)t * (unsigned)n;
+        int r = x >> 32 || total >> 32 ? (int)(x / total) : (int)((unsigned)x / (unsigned)total);
         while (begin_of(r + 1) <= t) ++r;
         while (begin_of(r) > t) --r;
         return r;
     }
 };
+
+// The unit of sequence `s` (whose blocks begin at `base`) that block t of the list belongs to.
+template <int RT, int BLK>
+__device__ inline Unit unit_in(const PagedAttendArgs& a, int s, long long base, long long t) {
+    const PagedSpan sp = paged_span(a.c, a.b, s);
+    const long long head = blocks_per_head<RT, BLK>(a, sp);
+    Unit u;
+    u.s = s; u.tok0 = sp.tok0; u.n = sp.n; u.len = sp.len;
+    const unsigned long long off = (unsigned long long)(t - base);
+    u.h = (off | head) >> 32 ? (int)(off / head) : (int)((unsigned)off / (unsigned)head);
+    u.base = base + u.h * head;
+    u.rt = 0;
+    unit_rows<RT, BLK>(a, u);
+    while (u.end() <= t) { u.base = u.end(); ++u.rt; unit_rows<RT, BLK>(a, u); }
+    return u;
+}
+
+// Parts of units in the workspace: two slots per range (the unit that it begins within, and the one that it
+// ends within).  O as float4: [row][D / 4], or with COLUMNS [D / 4][row] (a thread per row writes it); m and l per row.
+template <int RT, int D, bool COLUMNS>
+struct PartOf {
+    float* base;
+    __device__ PartOf(const PagedAttendArgs& a, int slot)
+        : base(reinterpret_cast<float*>(a.scratch + kPagedJoinBytes) + (size_t)slot * RT * (D + 2)) {}
+    __device__ float4* at(int row, int c4) const { return reinterpret_cast<float4*>(base) + (COLUMNS ? c4 * RT + row : row * (D / 4) + c4); }
+    __device__ float* m(int row) const { return base + RT * D + row; }
+    __device__ float* l(int row) const { return base + RT * (D + 1) + row; }
+};
+// What range r leaves for the join: the unit that begins in it and goes on behind it, whose parts are its own (at `slot`)
+// and the first ones of ranges r + 1 .. last.  last < 0: there is none.
+struct Join { Unit u; int slot, last; };
+__device__ inline Join* join_of(const PagedAttendArgs& a, int r) { return reinterpret_cast<Join*>(a.scratch) + r; }
+static_assert(sizeof(Join) * kPagedDecodeCtas <= kPagedJoinBytes, "joins");
+// Called with the last unit of a CTA's range.
+__device__ inline void leave_join(const PagedAttendArgs& a, const Range& rg, const Unit& u) {
+    Join* j = join_of(a, blockIdx.x);
+    const bool cut = u.base >= rg.t0 && u.end() > rg.t1;
+    if (cut) { j->u = u; j->slot = 2 * blockIdx.x + (rg.t0 < u.base ? 1 : 0); }
+    j->last = cut ? rg.of(u.end() - 1) : -1;
+}
+
+// Sums the list, cuts it into want(total) ranges (gridDim.x at most), and finds the unit that this CTA's range begins in.
+// For all threads of a block of THREADS; false (for all alike) where the CTA has no work, and no join then.
+struct FindShared { long long scan[32]; Unit unit; };
 template <int RT, int BLK, int THREADS, typename Want>
-__device__ inline bool find_range(const PagedAttendArgs& a, Range& r, Unit* first, long long* scan, Want want) {
+__device__ inline bool find_unit(const PagedAttendArgs& a, Range& rg, Unit& unit, FindShared& sh, Want want) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int per = (a.b.batch + THREADS - 1) / THREADS, s0 = min(a.b.batch, tid * per), s1 = min(a.b.batch, s0 + per);
+    const bool small = a.b.batch <= 32;   // every warp for itself, without meeting the others
+    const int per = small ? 1 : (a.b.batch + THREADS - 1) / THREADS, s0 = min(a.b.batch, (small ? lane : tid) * per), s1 = min(a.b.batch, s0 + per);
     long long mine = 0;
     for (int s = s0; s < s1; ++s) {
         const PagedSpan sp = paged_span(a.c, a.b, s);
@@ -105,41 +159,153 @@ __device__ inline bool find_range(const PagedAttendArgs& a, Range& r, Unit* firs
         const long long x = __shfl_up_sync(0xffffffffu, before, o);
         if (lane >= o) before += x;
     }
-    if (lane == 31) scan[warp] = before;
-    __syncthreads();
-    r.total = 0;
+    if (small) {
+        rg.total = __shfl_sync(0xffffffffu, before, 31);
+    } else {
+        if (lane == 31) sh.scan[warp] = before;
+        __syncthreads();
+        rg.total = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-        if (w < warp) before += scan[w];
-        r.total += scan[w];
+        for (int w = 0; w < THREADS / 32; ++w) {
+            if (w < warp) before += sh.scan[w];
+            rg.total += sh.scan[w];
+        }
     }
     before -= mine;
-    if (r.total == 0) return false;
-    r.n = (int)max(1ll, min((long long)gridDim.x, want(r.total)));
-    if (blockIdx.x >= r.n) return false;
-    r.t0 = r.begin_of(blockIdx.x);
-    r.t1 = r.begin_of(blockIdx.x + 1);
-    if (before <= r.t0 && r.t0 < before + mine) {
-        Unit u;
-        long long base = before;
-        for (int s = s0; s < s1; ++s) {
-            const PagedSpan sp = paged_span(a.c, a.b, s);
-            const long long head = blocks_per_head<RT, BLK>(a, sp), all = head * a.c.kv_heads;
-            if (r.t0 < base + all) {
-                u.s = s; u.tok0 = sp.tok0; u.n = sp.n; u.len = sp.len;
-                u.h = (int)((r.t0 - base) / head);
-                u.base = base + u.h * head;
-                u.rt = 0;
-                unit_rows<RT, BLK>(a, u);
-                while (u.end() <= r.t0) { u.base = u.end(); ++u.rt; unit_rows<RT, BLK>(a, u); }
-                break;
-            }
-            base += all;
-        }
-        *first = u;
+    rg.n = rg.total == 0 ? 0 : (int)max(1ll, min((long long)gridDim.x, want(rg.total)));
+    if ((int)blockIdx.x >= rg.n) {
+        if (tid == 0) join_of(a, blockIdx.x)->last = -1;
+        return false;
     }
-    __syncthreads();
+    rg.t0 = rg.begin_of(blockIdx.x);
+    rg.t1 = rg.begin_of(blockIdx.x + 1);
+    const long long t = rg.t0;
+    const bool here = before <= t && t < before + mine;
+    if (small) {
+        const int owner = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+        unit = unit_in<RT, BLK>(a, owner, __shfl_sync(0xffffffffu, before, owner), t);
+    } else {
+        if (here) {
+            long long base = before;
+            for (int s = s0; s < s1; ++s) {
+                const PagedSpan sp = paged_span(a.c, a.b, s);
+                const long long all = blocks_per_head<RT, BLK>(a, sp) * a.c.kv_heads;
+                if (t < base + all) { sh.unit = unit_in<RT, BLK>(a, s, base, t); break; }
+                base += all;
+            }
+        }
+        __syncthreads();
+        unit = sh.unit;
+    }
     return true;
+}
+
+// Four channels of a row's result: o / l, and the row's log-sum-exp with the first of them.
+template <int D>
+__device__ inline void store4(const PagedAttendArgs& a, const Unit& u, int row, int c, float4 o, float m, float l) {
+    const int r = u.row0 + row, j = r / a.c.group, h = u.h * a.c.group + (r - j * a.c.group);
+    const size_t at = (size_t)(u.tok0 + j) * a.c.q_heads + h;
+    // l is 0 where nothing was seen and NaN where a NaN was
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (a.c.out_f32) {
+        *reinterpret_cast<float4*>((float*)a.out + at * D + c) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    } else {
+        uint2 w;
+        w.x = ptx::pack_bf16x2(o.x * inv, o.y * inv);
+        w.y = ptx::pack_bf16x2(o.z * inv, o.w * inv);
+        *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + at * D + c) = w;
+    }
+    if (a.lse && c == 0) a.lse[at] = l == 0.f ? kPagedNegInf : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+__device__ inline float paged_ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// The second launch.  Block (r, y): joins the parts of the unit that begins in range r and goes on behind it.
+// One sequence may have dozens of parts of few rows: GROUPS groups of 256 threads take every GROUPS-th part each.  Units of
+// many rows have two or three: a thread takes PER positions instead, so that their loads go out together.
+template <int RT, int D, bool COLUMNS, int GROUPS, int PER>
+__global__ void __launch_bounds__(256 * GROUPS) paged_join_kernel(const PagedAttendArgs a) {
+    constexpr int kPos = RT * (D / 4);   // float4 positions of a part
+    __shared__ float4 so[GROUPS > 1 ? GROUPS - 1 : 1][256];
+    __shared__ float2 sml[GROUPS > 1 ? GROUPS - 1 : 1][256];
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
+    const Join* const jn = join_of(a, blockIdx.x);
+    const int c0 = blockIdx.x, c1 = jn->last, slot = jn->slot;
+    if (c1 < 0) return;
+    const Unit u = jn->u;
+    const int i = threadIdx.x & 255, g = threadIdx.x >> 8;
+    float m[PER], l[PER];
+    float4 o[PER];
+    int row[PER], c4[PER];
+    bool live[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int pos = (blockIdx.y * PER + k) * 256 + i;
+        row[k] = COLUMNS ? pos % RT : pos / (D / 4);
+        c4[k] = COLUMNS ? pos / RT : pos % (D / 4);
+        live[k] = pos < kPos && row[k] < u.rows;
+        m[k] = -FLT_MAX; l[k] = 0.f;
+        o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    auto add = [](float& m, float& l, float4& o, float pm, float pl, const float4& y) {
+        const float mn = fmaxf(m, pm), f0 = paged_ex2(m - mn), f = paged_ex2(pm - mn);
+        m = mn;
+        l = fmaf(pl, f, l * f0);
+        o.x = fmaf(y.x, f, o.x * f0); o.y = fmaf(y.y, f, o.y * f0); o.z = fmaf(y.z, f, o.z * f0); o.w = fmaf(y.w, f, o.w * f0);
+    };
+#pragma unroll (PER == 1 ? 4 : 1)
+    for (int x = c0 + g; x <= c1; x += GROUPS) {
+        const PartOf<RT, D, COLUMNS> p(a, x == c0 ? slot : 2 * x);
+        float pm[PER], pl[PER];
+        float4 y[PER];
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if (live[k]) { pm[k] = __ldcg(p.m(row[k])); pl[k] = __ldcg(p.l(row[k])); y[k] = __ldcg(p.at(row[k], c4[k])); }
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if (live[k]) add(m[k], l[k], o[k], pm[k], pl[k], y[k]);
+    }
+    if (GROUPS > 1) {
+        if (g > 0) { so[g - 1][i] = o[0]; sml[g - 1][i] = make_float2(m[0], l[0]); }
+        __syncthreads();
+        if (g > 0) return;
+#pragma unroll
+        for (int k = 0; k < GROUPS - 1; ++k) add(m[0], l[0], o[0], sml[k][i].x, sml[k][i].y, so[k][i]);
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+        if (live[k]) store4<D>(a, u, row[k], 4 * c4[k], o[k], m[k], l[k]);
+}
+
+// Launch that may begin while the kernel before it is still ending (every kernel of the paged cache waits for that one's
+// end before it touches memory).
+template <typename... P, typename... A>
+inline cudaError_t paged_launch(void (*fn)(P...), dim3 grid, int threads, int smem, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, fn, P(args)...);
+}
+// Opts a kernel in to its shared memory, once per device.
+template <typename F>
+inline cudaError_t paged_opt_in(std::atomic<unsigned long long>& done, F* fn, int smem, int device) {
+    const unsigned long long bit = device < 64 ? 1ull << device : 0;
+    if (bit && (done.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess && bit) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 
 }  // namespace mkv
