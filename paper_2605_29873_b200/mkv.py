@@ -405,6 +405,8 @@ class PagedKV:
         self.io_dtype = (MKV_F32 if kv_dtype == MKV_F32 else MKV_BF16) if io_dtype is None else io_dtype
         self.out_dtype = self.io_dtype if out_dtype is None else out_dtype
         self.device, self.pages = pages.device, pages
+        self._index, self._i32, self._f32 = pages.get_device(), torch.int32, torch.float32
+        self._current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
         self._io, self._out = (torch.bfloat16 if t == MKV_BF16 else torch.float32 for t in (self.io_dtype, self.out_dtype))
         page = paged_page_bytes(kv_heads, head_dim, page_size, kv_dtype)
         nbytes = paged_workspace_bytes(q_heads, kv_heads, head_dim, max_batch)
@@ -419,10 +421,9 @@ class PagedKV:
         off = (-self.workspace.data_ptr()) % 256
         torch.cuda.synchronize(self.device)
         ctx = C.c_void_p(0)
-        index = torch.cuda.current_device() if self.device.index is None else self.device.index
         _check(self._L.mkv_paged_create(self.layers, q_heads, kv_heads, head_dim, page_size, self.n_pages, max_batch, kv_dtype,
                                         self.io_dtype, self.out_dtype, _ptr(pages), size,
-                                        C.c_void_p(self.workspace.data_ptr() + off), nbytes, index, C.byref(ctx)),
+                                        C.c_void_p(self.workspace.data_ptr() + off), nbytes, self._index, C.byref(ctx)),
                "mkv_paged_create")
         self._ctx = ctx
 
@@ -437,35 +438,45 @@ class PagedKV:
         except Exception:
             pass
 
+    # The checks below run in front of every call; one call's launches take a few microseconds, so they ask each tensor
+    # for as little as they can.
     def _stream(self, stream):
-        return (self.torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream
+        return self._current_stream(self._index) if stream is None else stream.cuda_stream
 
     def _rows(self, x, heads):
         """Pointer of [tokens, heads, head_dim] and the elements from one token to the next."""
-        n, h, d = x.shape
+        d = self.head_dim
+        if x.dim() != 3 or x.dtype is not self._io or x.get_device() != self._index:
+            raise ValueError(f"expected [tokens, {heads}, {d}] {self._io} on {self.device}, got {tuple(x.shape)} {x.dtype} on {x.device}")
+        n, h, w = x.shape
+        if h != heads or w != d:
+            raise ValueError(f"expected [tokens, {heads}, {d}], got {tuple(x.shape)}")
         a, b, c = x.stride()
-        if h != heads or d != self.head_dim or x.dtype != self._io or x.device != self.device:
-            raise ValueError(f"expected [tokens, {heads}, {self.head_dim}] {self._io} on {self.device}, got {tuple(x.shape)} {x.dtype} on {x.device}")
-        if (d > 1 and c != 1) or (h > 1 and b != d):
+        if c != 1 or (b != d and h > 1):
             raise ValueError("heads and channels of a token must be contiguous")
         return x.data_ptr(), (a if n > 1 else heads * d)
 
     def _batch(self, n_tokens, lens, table, starts):
-        batch, i32 = lens.shape[0], self.torch.int32
-        if lens.dtype != i32 or table.dtype != i32 or lens.device != self.device or table.device != self.device:
+        batch, i32, index = lens.shape[0], self._i32, self._index
+        if lens.dtype is not i32 or table.dtype is not i32 or lens.get_device() != index or table.get_device() != index:
             raise ValueError("lens and table are int32 tensors of the cache's device")
-        if table.dim() != 2 or table.shape[0] != batch or table.stride(1) != 1 or not lens.is_contiguous():
-            raise ValueError("table is [batch, pages], its rows contiguous")
-        if starts is not None:
-            if starts.dtype != i32 or starts.device != self.device or starts.shape != (batch + 1,) or not starts.is_contiguous():
+        if table.dim() != 2 or table.shape[0] != batch or lens.dim() != 1 or not lens.is_contiguous():
+            raise ValueError("lens is [batch], table [batch, pages]")
+        a, b = table.stride()
+        if b != 1 and table.shape[1] > 1:
+            raise ValueError("a row of the table must be contiguous")
+        if starts is None:
+            if n_tokens != batch:
+                raise ValueError("without starts there is one new token per sequence")
+            sp = None
+        else:
+            if starts.dtype is not i32 or starts.get_device() != index or starts.shape != (batch + 1,) or not starts.is_contiguous():
                 raise ValueError("starts is an int32 [batch + 1] tensor of the cache's device")
-        elif n_tokens != batch:
-            raise ValueError("without starts there is one new token per sequence")
-        return batch, lens.data_ptr(), table.data_ptr(), (table.stride(0) if batch > 1 else table.shape[1]), \
-            (starts.data_ptr() if starts is not None else None)
+            sp = starts.data_ptr()
+        return batch, lens.data_ptr(), table.data_ptr(), (a if batch > 1 else table.shape[1]), sp
 
     def _dense(self, x, shape, dtype):
-        if tuple(x.shape) != shape or x.dtype != dtype or x.device != self.device or not x.is_contiguous():
+        if x.shape != shape or x.dtype is not dtype or x.get_device() != self._index or not x.is_contiguous():
             raise ValueError(f"expected a contiguous {shape} {dtype} tensor on {self.device}, got {tuple(x.shape)} {x.dtype} on {x.device}")
         return x.data_ptr()
 
@@ -485,7 +496,7 @@ class PagedKV:
         if v.shape[0] != n or (q is not None and q.shape[0] != n):
             raise ValueError("q, k and v have the same tokens")
         op = self._dense(q_out, (n, self.q_heads, self.head_dim), self._io) if q_out is not None else None
-        pos = self._dense(positions, (n,), self.torch.int32) if positions is not None else None
+        pos = self._dense(positions, (n,), self._i32) if positions is not None else None
         batch, lp, tp, stride, sp = self._batch(n, lens, table, starts)
         rc = self._L.mkv_paged_append(self._ctx, layer, qp, qs, kp, ks, vp, vs, op, n, batch, sp, lp, tp, stride, pos,
                                       self._stream(stream))
@@ -496,7 +507,7 @@ class PagedKV:
         n = q.shape[0]
         qp, qs = self._rows(q, self.q_heads)
         op = self._dense(out, (n, self.q_heads, self.head_dim), self._out)
-        ep = self._dense(lse, (n, self.q_heads), self.torch.float32) if lse is not None else None
+        ep = self._dense(lse, (n, self.q_heads), self._f32) if lse is not None else None
         batch, lp, tp, stride, sp = self._batch(n, lens, table, starts)
         rc = self._L.mkv_paged_attend(self._ctx, layer, qp, qs, op, ep, n, batch, sp, max_new, lp, tp, stride, scale, window,
                                       self._stream(stream))
@@ -509,7 +520,7 @@ class PagedKV:
         rows = K.shape[2]
         shape = (batch, self.kv_heads, rows, self.head_dim)
         kp, vp = self._dense(K, shape, self._io), self._dense(V, shape, self._io)
-        fp = self._dense(first, (batch,), self.torch.int32) if first is not None else None
+        fp = self._dense(first, (batch,), self._i32) if first is not None else None
         rc = self._L.mkv_paged_read(self._ctx, layer, batch, fp, lp, tp, stride, kp, vp, rows, self._stream(stream))
         if rc:
             raise MkvError(rc, "mkv_paged_read")
