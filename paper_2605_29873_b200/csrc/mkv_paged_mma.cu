@@ -54,7 +54,7 @@ struct Cfg {
     static constexpr int kStage = KIND == MKV_INT4 ? 16 * D + 128 * (D / 32) : 16 * D * (KIND == MKV_F32 ? 8 : 4);
     // bytes in flight per SM want 44 KB (6.5 TB/s x 1 us / 148): three stages of eight warps, of which one is read
     static constexpr int kStages = KIND == MKV_F32 && D == 128 ? 1 : KIND == MKV_INT4 || NT == 1 ? 3 : 2;
-    static constexpr int DP = D + 4;
+    static constexpr int DP = D + (KIND == MKV_BF16 && D == 128 && NT == 1 ? 0 : 4);   // the ring leaves no room for more there
     static constexpr int kRing = kW * kStages * kStage;
     static constexpr int kMerge = kW * RT * DP * 4;
     static constexpr int kMl = kW * RT * 8;
@@ -68,6 +68,19 @@ __device__ inline void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the same with nothing to add to
+__device__ inline void mma_f16_new(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ inline void mma_bf16_new(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ inline uint32_t pack_f16x2(float lo, float hi) {
     uint32_t r;
@@ -118,58 +131,34 @@ __device__ inline void rescale(State<D, NT>& st, const float (&sc)[NT], int lane
     }
 }
 
-// The softmax step of a block: s[token tile][..] in, p out.  What p will be multiplied by: token (x, e) of
-// the lane by 2^lv_of(x, e), no token of the lane by more than 2^lv.  The reference m moves when a
-// product could exceed 2^room; the largest is then 2^head.
-// EDGE: not every row sees every token of the block.
-template <int D, int NT, bool EDGE, typename LvOf>
-__device__ inline void softmax_step(State<D, NT>& st, float (&s)[2][4], const int (&pos)[NT], int window, int tok, float lv,
-                                    float room, float head, int lane, LvOf lv_of) {
-    // element (tile x, e) of row n: s[x][2 n + e], token tok + 8 x + 2 t + e
+// Takes the logits that a row does not see out of a block: element (tile x, e) of row n is s[x][2 n + e], token
+// tok + 8 x + 2 t + e.
+template <int NT>
+__device__ inline void hide(float (&s)[2][4], const int (&pos)[NT], int window, int tok, int lane) {
     const int t2 = tok + 2 * (lane & 3);
-    if (EDGE) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int hi = pos[n] - t2, lo = window > 0 ? hi - window : INT_MIN;
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    if (8 * x + e > hi || 8 * x + e <= lo) s[x][2 * n + e] = kPagedNegInf;
-        }
-    }
-    bool move = false;
-    float mx[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        mx[n] = fmaxf(fmaxf(s[0][2 * n], s[0][2 * n + 1]), fmaxf(s[1][2 * n], s[1][2 * n + 1])) + lv;
-        move |= mx[n] > st.m[n] + room;
-    }
-    if (__any_sync(kFull, move)) {
-        float sc[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            // token by token now: the largest logit and the largest factor may be different tokens'
-            mx[n] = fmaxf(fmaxf(s[0][2 * n] + lv_of(0, 0), s[0][2 * n + 1] + lv_of(0, 1)),
-                          fmaxf(s[1][2 * n] + lv_of(1, 0), s[1][2 * n + 1] + lv_of(1, 1)));
-            mx[n] = fmaxf(mx[n], __shfl_xor_sync(kFull, mx[n], 1));
-            mx[n] = fmaxf(mx[n], __shfl_xor_sync(kFull, mx[n], 2));
-            const float m = fmaxf(st.m[n], mx[n] - head);
-            sc[n] = ex2(st.m[n] - m);
-            st.m[n] = m;
-        }
-        rescale<D, NT>(st, sc, lane);
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
+        const int hi = pos[n] - t2, lo = window > 0 ? hi - window : INT_MIN;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float p = ex2(s[x][2 * n + e] - st.m[n]);
-                s[x][2 * n + e] = p;
-                st.l[n] += p;
-            }
+            for (int e = 0; e < 2; ++e)
+                if (8 * x + e > hi || 8 * x + e <= lo) s[x][2 * n + e] = kPagedNegInf;
+    }
+}
+// Moves the rows' references to mx (of this lane's tokens) - head, where that is higher.
+template <int D, int NT>
+__device__ inline void move_reference(State<D, NT>& st, float (&mx)[NT], float head, int lane) {
+    float sc[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        mx[n] = fmaxf(mx[n], __shfl_xor_sync(kFull, mx[n], 1));
+        mx[n] = fmaxf(mx[n], __shfl_xor_sync(kFull, mx[n], 2));
+        const float m = fmaxf(st.m[n], mx[n] - head);
+        sc[n] = ex2(st.m[n] - m);
+        st.m[n] = m;
+    }
+    rescale<D, NT>(st, sc, lane);
 }
 
 // ---- bf16 pages
@@ -213,7 +202,21 @@ __device__ inline void block_bf16(State<D, NT>& st, const QBf16<D, NT>& q, const
     for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int e = 0; e < 2 * NT; ++e) s[x][e] *= a.scale_log2;
-    softmax_step<D, NT, EDGE>(st, s, pos, a.window, tok, 0.f, 8.f, 0.f, lane, [](int, int) { return 0.f; });
+    if (EDGE) hide<NT>(s, pos, a.window, tok, lane);
+    float mx[NT];
+    bool move = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        mx[n] = fmaxf(fmaxf(s[0][2 * n], s[0][2 * n + 1]), fmaxf(s[1][2 * n], s[1][2 * n + 1]));
+        move |= mx[n] > st.m[n] + 8.f;
+    }
+    if (__any_sync(kFull, move)) move_reference<D, NT>(st, mx, 0.f, lane);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) st.l[n] += s[x][2 * n + e] = ex2(s[x][2 * n + e] - st.m[n]);
     uint32_t hi[NT][2], lo[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -392,47 +395,55 @@ __device__ inline void block_int4(State<D, NT>& st, const QInt4<D, NT, Q32>& q, 
     constexpr int NG = D / 32;
     const int g = lane >> 2, t = lane & 3;
     const uint32_t par = stage + 16 * D;
-    float s[2][4];
+    uint64_t s2[2][NT];   // pairs of neighbouring tokens
     // lowest * sum(q) first
     {
-        float x0[4] = {}, x1[4] = {};
+        float x0[4], x1[4];
         const uint32_t at = par + 32 * NG + (NG == 4 ? (t & 1) * 4 : 0);
         const uint32_t k0 = lds32(at + g * NG * 2), k1 = lds32(at + (g + 8) * NG * 2);
         const uint32_t a1 = NT == 2 ? q.sum[NT - 1][0] : 0u, a3 = NT == 2 ? q.sum[NT - 1][1] : 0u;
-        ptx::mma_bf16(x0, q.sum[0][0], a1, q.sum[0][1], a3, k0, k0);
-        ptx::mma_bf16(x1, q.sum[0][0], a1, q.sum[0][1], a3, k1, k1);
+        mma_bf16_new(x0, q.sum[0][0], a1, q.sum[0][1], a3, k0, k0);
+        mma_bf16_new(x1, q.sum[0][0], a1, q.sum[0][1], a3, k1, k1);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { s[0][e] = x0[e]; s[1][e] = x1[e]; }
+        for (int n = 0; n < NT; ++n) { s2[0][n] = pair(x0[2 * n], x0[2 * n + 1]); s2[1][n] = pair(x1[2 * n], x1[2 * n + 1]); }
     }
     const Words<NG> kw0 = lds_words<NG>(stage + g * (D / 2) + t * (4 * NG));
     const Words<NG> kw1 = lds_words<NG>(stage + (g + 8) * (D / 2) + t * (4 * NG));
     const Words<NG> ks0 = lds_words<NG>(par + t * (4 * NG)), ks1 = lds_words<NG>(par + (t + 4) * (4 * NG));
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
-        float x0[4] = {}, x1[4] = {};
+        float x0[4], x1[4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const uint32_t w0 = h ? kw0.w[j] >> 8 : kw0.w[j], w1 = h ? kw1.w[j] >> 8 : kw1.w[j];
             const uint32_t* qa = q.a[2 * j + h];
             constexpr int kRows = NT == 1 && !Q32 ? 1 : 2;
             const uint32_t a0 = qa[0], a1 = kRows == 2 ? qa[1] : 0u, a2 = qa[kRows], a3 = kRows == 2 ? qa[2 * kRows - 1] : 0u;
-            mma_f16(x0, a0, a1, a2, a3, w0 & 0x000f000fu, w0 & 0x00f000f0u);
-            mma_f16(x1, a0, a1, a2, a3, w1 & 0x000f000fu, w1 & 0x00f000f0u);
+            if (h == 0) {
+                mma_f16_new(x0, a0, a1, a2, a3, w0 & 0x000f000fu, w0 & 0x00f000f0u);
+                mma_f16_new(x1, a0, a1, a2, a3, w1 & 0x000f000fu, w1 & 0x00f000f0u);
+            } else {
+                mma_f16(x0, a0, a1, a2, a3, w0 & 0x000f000fu, w0 & 0x00f000f0u);
+                mma_f16(x1, a0, a1, a2, a3, w1 & 0x000f000fu, w1 & 0x00f000f0u);
+            }
         }
         if (Q32) { x0[0] += x0[2]; x0[1] += x0[3]; x1[0] += x1[2]; x1[1] += x1[3]; }
-        const float f00 = lo_bf16(ks0.w[j]), f01 = hi_bf16(ks0.w[j]), f10 = lo_bf16(ks1.w[j]), f11 = hi_bf16(ks1.w[j]);
+        const uint64_t f0 = pair(lo_bf16(ks0.w[j]), hi_bf16(ks0.w[j])), f1 = pair(lo_bf16(ks1.w[j]), hi_bf16(ks1.w[j]));
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            s[0][2 * n] = fmaf(f00, x0[2 * n], s[0][2 * n]);
-            s[0][2 * n + 1] = fmaf(f01, x0[2 * n + 1], s[0][2 * n + 1]);
-            s[1][2 * n] = fmaf(f10, x1[2 * n], s[1][2 * n]);
-            s[1][2 * n + 1] = fmaf(f11, x1[2 * n + 1], s[1][2 * n + 1]);
+            s2[0][n] = fma2(f0, pair(x0[2 * n], x0[2 * n + 1]), s2[0][n]);
+            s2[1][n] = fma2(f1, pair(x1[2 * n], x1[2 * n + 1]), s2[1][n]);
         }
     }
+    float s[2][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) { s[x][2 * n] *= q.back[n]; s[x][2 * n + 1] *= q.back[n]; }
+        for (int x = 0; x < 2; ++x) {
+            const float2 y = unpair(mul2(s2[x][n], pair(q.back[n], q.back[n])));
+            s[x][2 * n] = y.x; s[x][2 * n + 1] = y.y;
+        }
+    if (EDGE) hide<NT>(s, pos, a.window, tok, lane);
 
     Words<NG> vs0 = lds_words<NG>(par + 64 * NG + t * (4 * NG)), vs1 = lds_words<NG>(par + 64 * NG + (t + 4) * (4 * NG));
     uint32_t keep0 = kFull, keep1 = kFull;
@@ -445,9 +456,7 @@ __device__ inline void block_int4(State<D, NT>& st, const QInt4<D, NT, Q32>& q, 
 #pragma unroll
         for (int j = 0; j < NG; ++j) { vs0.w[j] &= keep0; vs1.w[j] &= keep1; }
     }
-    // log2 of the largest scale of this lane's tokens, rounded up (a NaN is passed over), kept where both p and
-    // p * scale are far from the ends of their ranges
-    auto log2_up = [](float x) { return x > 0.f ? (float)min(max((int)(__float_as_uint(x) >> 23) - 126, -88), 104) : -88.f; };
+    // the largest scale of every token of this lane (a NaN is passed over)
     __nv_bfloat162 big0 = *(const __nv_bfloat162*)&vs0.w[0], big1 = *(const __nv_bfloat162*)&vs1.w[0];
 #pragma unroll
     for (int j = 1; j < NG; ++j) {
@@ -455,11 +464,38 @@ __device__ inline void block_int4(State<D, NT>& st, const QInt4<D, NT, Q32>& q, 
         big1 = __hmax2(big1, *(const __nv_bfloat162*)&vs1.w[j]);
     }
     const __nv_bfloat162 big = __hmax2(big0, big1);
-    softmax_step<D, NT, EDGE>(st, s, pos, a.window, tok, log2_up(fmaxf(__low2float(big), __high2float(big))), 12.f, 4.f, lane,
-                              [&](int x, int e) {
-                                  const __nv_bfloat162 y = x ? big1 : big0;
-                                  return log2_up(e ? __high2float(y) : __low2float(y));
-                              });
+    // p, and whether p * scale stays within fp16, as far as the largest p and the largest scale say (2^-88: p is kept within
+    // fp32 even where the scales are nothing)
+    const float bigf = fmaxf(fmaxf(__low2float(big), __high2float(big)), 3.2e-27f);
+    float p[2][4];
+    bool move = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) p[x][2 * n + e] = ex2(s[x][2 * n + e] - st.m[n]);
+        move |= fmaxf(fmaxf(p[0][2 * n], p[0][2 * n + 1]), fmaxf(p[1][2 * n], p[1][2 * n + 1])) * bigf > 4096.f;
+    }
+    if (__any_sync(kFull, move)) {
+        // token by token now: the largest p and the largest scale may be different tokens'.  The reference goes to where the
+        // largest product is 2^4.
+        auto log2_up = [](float x) { return x > 0.f ? (float)min(max((int)(__float_as_uint(x) >> 23) - 126, -88), 104) : -88.f; };
+        float mx[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            mx[n] = fmaxf(fmaxf(s[0][2 * n] + log2_up(__low2float(big0)), s[0][2 * n + 1] + log2_up(__high2float(big0))),
+                          fmaxf(s[1][2 * n] + log2_up(__low2float(big1)), s[1][2 * n + 1] + log2_up(__high2float(big1))));
+        move_reference<D, NT>(st, mx, 4.f, lane);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) p[x][2 * n + e] = ex2(s[x][2 * n + e] - st.m[n]);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) st.l[n] += (p[0][2 * n] + p[0][2 * n + 1]) + (p[1][2 * n] + p[1][2 * n + 1]);
 
     // lowest values: p as two bf16; rows of the operand beyond the groups repeat them and are not read
     {
@@ -468,9 +504,9 @@ __device__ inline void block_int4(State<D, NT>& st, const QInt4<D, NT, Q32>& q, 
         if (EDGE) { l0 &= keep0; l1 &= keep1; }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const uint32_t h0 = ptx::pack_bf16x2(s[0][2 * n], s[0][2 * n + 1]), h1 = ptx::pack_bf16x2(s[1][2 * n], s[1][2 * n + 1]);
-            const uint32_t r0 = ptx::pack_bf16x2(s[0][2 * n] - lo_bf16(h0), s[0][2 * n + 1] - hi_bf16(h0));
-            const uint32_t r1 = ptx::pack_bf16x2(s[1][2 * n] - lo_bf16(h1), s[1][2 * n + 1] - hi_bf16(h1));
+            const uint32_t h0 = ptx::pack_bf16x2(p[0][2 * n], p[0][2 * n + 1]), h1 = ptx::pack_bf16x2(p[1][2 * n], p[1][2 * n + 1]);
+            const uint32_t r0 = ptx::pack_bf16x2(p[0][2 * n] - lo_bf16(h0), p[0][2 * n + 1] - hi_bf16(h0));
+            const uint32_t r1 = ptx::pack_bf16x2(p[1][2 * n] - lo_bf16(h1), p[1][2 * n + 1] - hi_bf16(h1));
             ptx::mma_bf16(st.lowest[n], l0, 0u, l1, 0u, h0, h1);
             ptx::mma_bf16(st.lowest[n], l0, 0u, l1, 0u, r0, r1);
         }
@@ -478,17 +514,18 @@ __device__ inline void block_int4(State<D, NT>& st, const QInt4<D, NT, Q32>& q, 
     const Words<NG> vw0 = lds_words<NG>(stage + 8 * D + t * D + g * (4 * NG)), vw1 = lds_words<NG>(stage + 8 * D + (t + 4) * D + g * (4 * NG));
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
-        const float f00 = lo_bf16(vs0.w[j]), f01 = hi_bf16(vs0.w[j]), f10 = lo_bf16(vs1.w[j]), f11 = hi_bf16(vs1.w[j]);
+        const uint64_t f0 = pair(lo_bf16(vs0.w[j]), hi_bf16(vs0.w[j])), f1 = pair(lo_bf16(vs1.w[j]), hi_bf16(vs1.w[j]));
         uint32_t b[NT][2], bl[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float y[4] = {s[0][2 * n] * f00, s[0][2 * n + 1] * f01, s[1][2 * n] * f10, s[1][2 * n + 1] * f11};
+            const float2 y0 = unpair(mul2(pair(p[0][2 * n], p[0][2 * n + 1]), f0)), y1 = unpair(mul2(pair(p[1][2 * n], p[1][2 * n + 1]), f1));
+            float y[4] = {y0.x, y0.y, y1.x, y1.y};
             if (EDGE) {
                 // the scale of a token that a row does not see may be NaN
-                if (s[0][2 * n] == 0.f) y[0] = 0.f;
-                if (s[0][2 * n + 1] == 0.f) y[1] = 0.f;
-                if (s[1][2 * n] == 0.f) y[2] = 0.f;
-                if (s[1][2 * n + 1] == 0.f) y[3] = 0.f;
+                if (p[0][2 * n] == 0.f) y[0] = 0.f;
+                if (p[0][2 * n + 1] == 0.f) y[1] = 0.f;
+                if (p[1][2 * n] == 0.f) y[2] = 0.f;
+                if (p[1][2 * n + 1] == 0.f) y[3] = 0.f;
             }
             b[n][0] = pack_f16x2(y[0], y[1]);
             b[n][1] = pack_f16x2(y[2], y[3]);
@@ -631,7 +668,7 @@ __device__ inline void put_state(StateF32<D>& st, float* o, float2* ml, int lane
 // A warp's state into its slot of the merge buffer: O [RT][D + 4], and (m, l) per row.
 template <int KIND, int D, int NT>
 __device__ inline void put_state(State<D, NT>& st, float* o, float2* ml, int lane) {
-    constexpr int DP = D + 4, NG = D / 32;
+    constexpr int DP = Cfg<KIND, D, NT>::DP, NG = D / 32;
     const int g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -698,6 +735,8 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
     extern __shared__ uint8_t raw_smem[];
     __shared__ __align__(8) unsigned long long bars[kW * C::kStages];
     __shared__ FindShared fs;
+    __shared__ Unit s_unit, s_fetch[kW];
+    __shared__ Range s_range;
     uint8_t* const smem = raw_smem + ((1024u - (ptx::smem_u32(raw_smem) & 1023u)) & 1023u);
     float* const merge = reinterpret_cast<float*>(smem + C::kRing);
     float2* const mls = reinterpret_cast<float2*>(smem + C::kRing + C::kMerge);
@@ -709,63 +748,82 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
     }
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    Range rg;
-    Unit f;
-    if (!find_unit<RT, 16, kThreads>(a, rg, f, fs, want)) return;
-    const long long t0 = rg.t0, t1 = rg.t1;
-    __syncthreads();   // the barriers are ready
+    // The units lie in shared memory, the CTA's and the one that each warp fetches from: the loops below need little of them.
+    {
+        Range rg;
+        Unit first;
+        if (!find_unit<RT, 16, kThreads>(a, rg, first, fs, want)) return;
+        if (lane == 0) s_fetch[warp] = first;
+        if (tid == 0) { s_unit = first; s_range = rg; }
+    }
+    __syncthreads();   // and the barriers are ready
 
-    // ---- this warp's fetches: unit f, blocks f_lo + warp, + kW, ... of its part [f_lo, f_hi) in the range
+    // ---- this warp's fetches: blocks warp, warp + kW, ... of every unit's part in the range.  The addresses of the next
+    // 32, one per lane:
     const uint32_t ring = ptx::smem_u32(smem) + warp * C::kStages * C::kStage;
     const uint32_t bar0 = ptx::smem_u32(&bars[warp * C::kStages]);
-    Unit u = f;
+    using Where = typename std::conditional<KIND == MKV_BF16, int, unsigned long long>::type;   // a row of all pages', or an address
+    Where where = 0;
+    int f_next = warp, f_have = 0, f_at = 0, f_stage = 0, in_flight = 0;
     bool more = true;
-    int f_i = warp, f_n, f_first, page_of = 0, f_stage = 0, in_flight = 0;
-    auto enter = [&]() {
-        const long long lo = max(f.base, t0), hi = min(f.end(), t1);
-        f_first = f.blk0 + (int)(lo - f.base);
-        f_n = f.nblk == 0 ? 0 : (int)(hi - lo);
-        f_i = warp;
+    auto refill = [&]() {
+        Unit f = s_fetch[warp];
+        const long long t0 = s_range.t0, t1 = s_range.t1;
+        f_have = f_at = 0;
+        for (;;) {
+            const long long lo = max(f.base, t0), hi = min(f.end(), t1);
+            const int n = f.nblk == 0 ? 0 : (int)(hi - lo);
+            if (f_next < n) {
+                const int i = f_next + lane * kW, pos = (f.blk0 + (int)(lo - f.base) + i) << 4;
+                if (i < n) {
+                    const int page = paged_page(a.c, a.b, f.s, pos), row = pos & ((1 << a.c.page_shift) - 1);
+                    if (KIND == MKV_BF16)
+                        where = (Where)(layer_rows + (long long)page * 2 * (a.c.kv_heads << a.c.page_shift) + (f.h << a.c.page_shift) + row);
+                    else
+                        where = (Where)(a.c.pages + (size_t)page * a.c.page_bytes + (size_t)f.h * a.c.head_bytes +
+                                        (KIND == MKV_INT4 ? (size_t)(row >> 4) * C::kStage : (size_t)row * (D * 4)));
+                }
+                f_have = min(32, (n - f_next + kW - 1) / kW);
+                f_next += 32 * kW;
+                break;
+            }
+            if (f.end() >= t1) { more = false; break; }
+            next_unit<RT, 16>(a, f);
+            f_next = warp;
+        }
+        __syncwarp();
+        if (lane == 0) s_fetch[warp] = f;
+        __syncwarp();
     };
     // one more block on its way, if there is one
     auto fetch = [&]() {
-        while (more && f_i >= f_n) {
-            if (f.end() >= t1 || !next_unit<RT, 16>(a, f)) more = false;
-            else enter();
+        if (f_at == f_have) {
+            if (!more) return;
+            refill();
+            if (f_have == 0) return;
         }
-        if (!more) return;
-        const int k = (f_i - warp) / kW;
-        if ((k & 31) == 0) {   // pages of the next 32 blocks, one per lane
-            const int i = f_i + lane * kW;
-            page_of = i < f_n ? paged_page(a.c, a.b, f.s, (f_first + i) << 4) : 0;
-        }
-        const int page = __shfl_sync(kFull, page_of, k & 31);
-        const int row = ((f_first + f_i) << 4) & ((1 << a.c.page_shift) - 1);
+        const Where at = __shfl_sync(kFull, where, f_at);
+        ++f_at;
         if (lane == 0) {
             const uint32_t dst = ring + f_stage * C::kStage, bar = bar0 + f_stage * 8;
             ptx::mbar_arrive_expect_tx(bar, C::kStage);
             if (KIND == MKV_INT4) {
-                ptx::bulk_g2s(dst, a.c.pages + (size_t)page * a.c.page_bytes + (size_t)f.h * a.c.head_bytes + (size_t)(row >> 4) * C::kStage,
-                              C::kStage, bar);
+                ptx::bulk_g2s(dst, (const void*)(size_t)at, C::kStage, bar);
             } else if (KIND == MKV_F32) {
-                const uint8_t* src = a.c.pages + (size_t)page * a.c.page_bytes + (size_t)f.h * a.c.head_bytes + (size_t)row * (D * 4);
-                ptx::bulk_g2s(dst, src, C::kStage / 2, bar);
-                ptx::bulk_g2s(dst + C::kStage / 2, src + a.c.kv_bytes, C::kStage / 2, bar);
+                ptx::bulk_g2s(dst, (const void*)(size_t)at, C::kStage / 2, bar);
+                ptx::bulk_g2s(dst + C::kStage / 2, (const uint8_t*)(size_t)at + a.c.kv_bytes, C::kStage / 2, bar);
             } else {
                 const int kv = a.c.kv_heads << a.c.page_shift;
-                const int y = (int)(layer_rows + (long long)page * 2 * kv) + (f.h << a.c.page_shift) + row;
 #pragma unroll
                 for (int c = 0; c < D / 64; ++c) {
-                    tma_2d(dst + c * 2048, &map, 64 * c, y, bar);
-                    tma_2d(dst + 16 * D * 2 + c * 2048, &map, 64 * c, y + kv, bar);
+                    tma_2d(dst + c * 2048, &map, 64 * c, (int)at, bar);
+                    tma_2d(dst + 16 * D * 2 + c * 2048, &map, 64 * c, (int)at + kv, bar);
                 }
             }
         }
         f_stage = f_stage + 1 == C::kStages ? 0 : f_stage + 1;
         ++in_flight;
-        f_i += kW;
     };
-    enter();
 #pragma unroll 1
     for (int i = 0; i < C::kStages; ++i) fetch();
 
@@ -774,8 +832,15 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
     int stage = 0, parity = 0;
     bool ok = true;
     for (;;) {
-        const long long lo = max(u.base, t0), hi = min(u.end(), t1);
-        const int first = u.blk0 + (int)(lo - u.base), cnt = u.nblk == 0 ? 0 : (int)(hi - lo);
+        const Unit& u = s_unit;
+        int first, cnt, full_lo, full_hi;   // blocks of the unit in the range; those that all rows see whole
+        {
+            const long long lo = max(u.base, s_range.t0), hi = min(u.end(), s_range.t1);
+            first = u.blk0 + (int)(lo - u.base);
+            cnt = u.nblk == 0 ? 0 : (int)(hi - lo);
+            full_hi = (u.plo + 1) >> 4;
+            full_lo = a.window > 0 ? ((u.phi - a.window) >> 4) + 1 : 0;
+        }
         int pos[NT];
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
@@ -794,7 +859,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
                 ok = __all_sync(kFull, ok);
                 if (!ok) continue;   // the result is lost; what is on its way is waited for at the end
                 const int tok = (first + i) << 4;
-                const bool edge = tok + 15 > u.plo || (a.window > 0 && tok <= u.phi - a.window);
+                const bool edge = first + i >= full_hi || first + i < full_lo;
                 const uint32_t at = ring + stage * C::kStage;
                 if constexpr (KIND == MKV_INT4) {
                     if (edge) block_int4<D, NT, Q32, HL, true>(st, q, a, u, pos, at, tok, lane);
@@ -817,8 +882,8 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
         else put_state<KIND, D, NT>(st, merge + warp * RT * DP, mls + warp * RT, lane);
         __syncthreads();
         // ---- the warps' states become one
-        const bool whole = lo == u.base && hi == u.end();
-        const PartOf<RT, D, false> part(a, 2 * blockIdx.x + (t0 < u.base ? 1 : 0));
+        const bool whole = s_range.t0 <= u.base && u.end() <= s_range.t1;
+        const PartOf<RT, D, false> part(a, 2 * blockIdx.x + (s_range.t0 < u.base ? 1 : 0));
         for (int i = tid; i < RT * (D / 4); i += kThreads) {
             const int row = i / (D / 4), c = (i - row * (D / 4)) * 4;
             float m = -FLT_MAX, l = 0.f;
@@ -840,11 +905,14 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
                 if (c == 0) { *part.m(row) = m; *part.l(row) = l; }
             }
         }
-        if (u.end() >= t1) break;
-        next_unit<RT, 16>(a, u);
-        __syncthreads();   // the merge buffer is free again
+        if (u.end() >= s_range.t1) break;
+        Unit next = u;
+        next_unit<RT, 16>(a, next);
+        __syncthreads();   // the merge buffer is free again, and the unit has been read
+        if (tid == 0) s_unit = next;
+        __syncthreads();
     }
-    if (tid == 0) leave_join(a, rg, u);
+    if (tid == 0) leave_join(a, s_range, s_unit);
     // copies still on their way after a wait that ran out
     while (in_flight > 0) {
         paged_wait(bar0 + stage * 8, parity);
