@@ -134,11 +134,12 @@ __device__ inline void rescale(State<D, NT>& st, const float (&sc)[NT], int lane
 // Takes the logits that a row does not see out of a block: element (tile x, e) of row n is s[x][2 n + e], token
 // tok + 8 x + 2 t + e.
 template <int NT>
-__device__ inline void hide(float (&s)[2][4], const int (&pos)[NT], int window, int tok, int lane) {
+__device__ inline void hide(float (&s)[2][4], const PagedAttendArgs& a, const Unit& u, int tok, int lane) {
     const int t2 = tok + 2 * (lane & 3);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int hi = pos[n] - t2, lo = window > 0 ? hi - window : INT_MIN;
+        const int pos = u.len - u.n + (u.row0 + min((lane >> 2) + 8 * n, u.rows - 1)) / a.c.group;
+        const int hi = pos - t2, lo = a.window > 0 ? hi - a.window : INT_MIN;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -185,7 +186,7 @@ __device__ inline void load_q(const PagedAttendArgs& a, const Unit& u, QBf16<D, 
 
 template <int D, int NT, bool EDGE>
 __device__ inline void block_bf16(State<D, NT>& st, const QBf16<D, NT>& q, const PagedAttendArgs& a, const Unit& u,
-                                  const int (&pos)[NT], uint32_t stage, int tok, int lane) {
+                                  uint32_t stage, int tok, int lane) {
     // tiles of 16 rows x 64 channels, 128-byte rows, 16-byte chunk c of row r at c ^ (r & 7)
     const int r = (lane & 7) + ((lane >> 4) << 3), c0 = (lane >> 3) & 1;
     const uint32_t row = stage + r * 128;
@@ -202,7 +203,7 @@ __device__ inline void block_bf16(State<D, NT>& st, const QBf16<D, NT>& q, const
     for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int e = 0; e < 2 * NT; ++e) s[x][e] *= a.scale_log2;
-    if (EDGE) hide<NT>(s, pos, a.window, tok, lane);
+    if (EDGE) hide<NT>(s, a, u, tok, lane);
     float mx[NT];
     bool move = false;
 #pragma unroll
@@ -391,7 +392,7 @@ __device__ inline void load_q(const PagedAttendArgs& a, const Unit& u, QInt4<D, 
 
 template <int D, int NT, bool Q32, bool HL, bool EDGE>
 __device__ inline void block_int4(State<D, NT>& st, const QInt4<D, NT, Q32>& q, const PagedAttendArgs& a, const Unit& u,
-                                  const int (&pos)[NT], uint32_t stage, int tok, int lane) {
+                                  uint32_t stage, int tok, int lane) {
     constexpr int NG = D / 32;
     const int g = lane >> 2, t = lane & 3;
     const uint32_t par = stage + 16 * D;
@@ -435,15 +436,35 @@ __device__ inline void block_int4(State<D, NT>& st, const QInt4<D, NT, Q32>& q, 
             s2[1][n] = fma2(f1, pair(x1[2 * n], x1[2 * n + 1]), s2[1][n]);
         }
     }
-    float s[2][4];
+    // s2 * back are the logits; p = 2^(s2 * back - m)
+    auto logits = [&](float (&s)[2][4]) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const float2 y = unpair(mul2(s2[x][n], pair(q.back[n], q.back[n])));
-            s[x][2 * n] = y.x; s[x][2 * n + 1] = y.y;
+            for (int x = 0; x < 2; ++x) {
+                const float2 y = unpair(mul2(s2[x][n], pair(q.back[n], q.back[n])));
+                s[x][2 * n] = y.x; s[x][2 * n + 1] = y.y;
+            }
+        if (EDGE) hide<NT>(s, a, u, tok, lane);
+    };
+    float p[2][4];
+    auto weights = [&]() {
+        if (EDGE) {
+            logits(p);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) { p[x][2 * n] = ex2(p[x][2 * n] - st.m[n]); p[x][2 * n + 1] = ex2(p[x][2 * n + 1] - st.m[n]); }
+        } else {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const float2 y = unpair(fma2(s2[x][n], pair(q.back[n], q.back[n]), pair(-st.m[n], -st.m[n])));
+                    p[x][2 * n] = ex2(y.x); p[x][2 * n + 1] = ex2(y.y);
+                }
         }
-    if (EDGE) hide<NT>(s, pos, a.window, tok, lane);
+    };
 
     Words<NG> vs0 = lds_words<NG>(par + 64 * NG + t * (4 * NG)), vs1 = lds_words<NG>(par + 64 * NG + (t + 4) * (4 * NG));
     uint32_t keep0 = kFull, keep1 = kFull;
@@ -467,32 +488,23 @@ __device__ inline void block_int4(State<D, NT>& st, const QInt4<D, NT, Q32>& q, 
     // p, and whether p * scale stays within fp16, as far as the largest p and the largest scale say (2^-88: p is kept within
     // fp32 even where the scales are nothing)
     const float bigf = fmaxf(fmaxf(__low2float(big), __high2float(big)), 3.2e-27f);
-    float p[2][4];
+    weights();
     bool move = false;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) p[x][2 * n + e] = ex2(s[x][2 * n + e] - st.m[n]);
+    for (int n = 0; n < NT; ++n)
         move |= fmaxf(fmaxf(p[0][2 * n], p[0][2 * n + 1]), fmaxf(p[1][2 * n], p[1][2 * n + 1])) * bigf > 4096.f;
-    }
     if (__any_sync(kFull, move)) {
         // token by token now: the largest p and the largest scale may be different tokens'.  The reference goes to where the
         // largest product is 2^4.
         auto log2_up = [](float x) { return x > 0.f ? (float)min(max((int)(__float_as_uint(x) >> 23) - 126, -88), 104) : -88.f; };
-        float mx[NT];
+        float mx[NT], s[2][4];
+        logits(s);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
             mx[n] = fmaxf(fmaxf(s[0][2 * n] + log2_up(__low2float(big0)), s[0][2 * n + 1] + log2_up(__high2float(big0))),
                           fmaxf(s[1][2 * n] + log2_up(__low2float(big1)), s[1][2 * n + 1] + log2_up(__high2float(big1))));
         move_reference<D, NT>(st, mx, 4.f, lane);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) p[x][2 * n + e] = ex2(s[x][2 * n + e] - st.m[n]);
+        weights();
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) st.l[n] += (p[0][2 * n] + p[0][2 * n + 1]) + (p[1][2 * n] + p[1][2 * n + 1]);
@@ -578,9 +590,10 @@ __device__ inline void load_q(const PagedAttendArgs& a, const Unit& u, QF32<D>& 
 }
 
 template <int D, bool EDGE>
-__device__ inline void block_f32(StateF32<D>& st, const QF32<D>& q, const PagedAttendArgs& a, const Unit& u, int pos, uint32_t stage,
+__device__ inline void block_f32(StateF32<D>& st, const QF32<D>& q, const PagedAttendArgs& a, const Unit& u, uint32_t stage,
                                  uint32_t weights, int tok, int lane) {
     constexpr int CPL = D / 32;
+    const int pos = EDGE ? u.len - u.n + (u.row0 + min(lane & 7, u.rows - 1)) / a.c.group : 0;
     float s[4];
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
@@ -762,10 +775,8 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
     // 32, one per lane:
     const uint32_t ring = ptx::smem_u32(smem) + warp * C::kStages * C::kStage;
     const uint32_t bar0 = ptx::smem_u32(&bars[warp * C::kStages]);
-    using Where = typename std::conditional<KIND == MKV_BF16, int, unsigned long long>::type;   // a row of all pages', or an address
-    Where where = 0;
-    int f_next = warp, f_have = 0, f_at = 0, f_stage = 0, in_flight = 0;
-    bool more = true;
+    unsigned where = 0;   // as a row of all pages (bf16), or in blocks of the layer
+    int f_next = warp, f_have = 0, f_at = 0;   // f_next < 0: there are no more
     auto refill = [&]() {
         Unit f = s_fetch[warp];
         const long long t0 = s_range.t0, t1 = s_range.t1;
@@ -777,17 +788,15 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
                 const int i = f_next + lane * kW, pos = (f.blk0 + (int)(lo - f.base) + i) << 4;
                 if (i < n) {
                     const int page = paged_page(a.c, a.b, f.s, pos), row = pos & ((1 << a.c.page_shift) - 1);
-                    if (KIND == MKV_BF16)
-                        where = (Where)(layer_rows + (long long)page * 2 * (a.c.kv_heads << a.c.page_shift) + (f.h << a.c.page_shift) + row);
-                    else
-                        where = (Where)(a.c.pages + (size_t)page * a.c.page_bytes + (size_t)f.h * a.c.head_bytes +
-                                        (KIND == MKV_INT4 ? (size_t)(row >> 4) * C::kStage : (size_t)row * (D * 4)));
+                    const unsigned heads = KIND == MKV_INT4 ? a.c.kv_heads : 2 * a.c.kv_heads;   // of a page, K and V
+                    if (KIND == MKV_BF16) where = (unsigned)layer_rows + ((page * heads + f.h) << a.c.page_shift) + row;
+                    else where = ((page * heads + f.h) << (a.c.page_shift - 4)) + (row >> 4);
                 }
                 f_have = min(32, (n - f_next + kW - 1) / kW);
                 f_next += 32 * kW;
                 break;
             }
-            if (f.end() >= t1) { more = false; break; }
+            if (f.end() >= t1) { f_next = -1; break; }
             next_unit<RT, 16>(a, f);
             f_next = warp;
         }
@@ -795,23 +804,24 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
         if (lane == 0) s_fetch[warp] = f;
         __syncwarp();
     };
-    // one more block on its way, if there is one
-    auto fetch = [&]() {
+    // one more block on its way into stage `to`, if there is one
+    auto fetch = [&](int to) {
         if (f_at == f_have) {
-            if (!more) return;
+            if (f_next < 0) return;
             refill();
             if (f_have == 0) return;
         }
-        const Where at = __shfl_sync(kFull, where, f_at);
+        const unsigned at = __shfl_sync(kFull, where, f_at);
         ++f_at;
         if (lane == 0) {
-            const uint32_t dst = ring + f_stage * C::kStage, bar = bar0 + f_stage * 8;
+            const uint32_t dst = ring + to * C::kStage, bar = bar0 + to * 8;
             ptx::mbar_arrive_expect_tx(bar, C::kStage);
             if (KIND == MKV_INT4) {
-                ptx::bulk_g2s(dst, (const void*)(size_t)at, C::kStage, bar);
+                ptx::bulk_g2s(dst, a.c.pages + (size_t)at * C::kStage, C::kStage, bar);
             } else if (KIND == MKV_F32) {
-                ptx::bulk_g2s(dst, (const void*)(size_t)at, C::kStage / 2, bar);
-                ptx::bulk_g2s(dst + C::kStage / 2, (const uint8_t*)(size_t)at + a.c.kv_bytes, C::kStage / 2, bar);
+                const uint8_t* src = a.c.pages + (size_t)at * (C::kStage / 2);
+                ptx::bulk_g2s(dst, src, C::kStage / 2, bar);
+                ptx::bulk_g2s(dst + C::kStage / 2, src + a.c.kv_bytes, C::kStage / 2, bar);
             } else {
                 const int kv = a.c.kv_heads << a.c.page_shift;
 #pragma unroll
@@ -821,61 +831,50 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
                 }
             }
         }
-        f_stage = f_stage + 1 == C::kStages ? 0 : f_stage + 1;
-        ++in_flight;
     };
 #pragma unroll 1
-    for (int i = 0; i < C::kStages; ++i) fetch();
+    for (int i = 0; i < C::kStages; ++i) fetch(i);
 
     // ---- units of the range
     typename std::conditional<KIND == MKV_F32, StateF32<D>, State<D, NT>>::type st;
+    const uint32_t weights = ptx::smem_u32(smem) + C::kRing + C::kMerge + C::kMl + warp * 512;   // fp32 pages
     int stage = 0, parity = 0;
     bool ok = true;
     for (;;) {
         const Unit& u = s_unit;
-        int first, cnt, full_lo, full_hi;   // blocks of the unit in the range; those that all rows see whole
+        int cnt, full_lo, full_n;   // blocks of the unit in the range; the first that all rows see whole, and how many
         {
             const long long lo = max(u.base, s_range.t0), hi = min(u.end(), s_range.t1);
-            first = u.blk0 + (int)(lo - u.base);
+            const int first = u.blk0 + (int)(lo - u.base);
             cnt = u.nblk == 0 ? 0 : (int)(hi - lo);
-            full_hi = (u.plo + 1) >> 4;
-            full_lo = a.window > 0 ? ((u.phi - a.window) >> 4) + 1 : 0;
-        }
-        int pos[NT];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            const int row = KIND == MKV_F32 ? lane & 7 : (lane >> 2) + 8 * i;
-            pos[i] = u.len - u.n + (u.row0 + min(row, u.rows - 1)) / a.c.group;
+            full_lo = max(0, (a.window > 0 ? ((u.phi - a.window) >> 4) + 1 : 0) - first);
+            full_n = max(0, ((u.plo + 1) >> 4) - first - full_lo);
         }
         clear(st);
-        if (warp < cnt) {
+        if (warp < cnt && ok) {
             typename std::conditional<KIND == MKV_INT4, QInt4<D, NT, Q32>, typename std::conditional<KIND == MKV_F32, QF32<D>, QBf16<D, NT>>::type>::type q;
             load_q(a, u, q, lane);
+#pragma unroll 1
             for (int i = warp; i < cnt; i += kW) {
-                if (ok && !paged_wait(bar0 + stage * 8, parity)) {
-                    ok = false;
+                ok = __all_sync(kFull, paged_wait(bar0 + stage * 8, parity));
+                if (!ok) {
                     if (lane == 0) paged_fail(a.c, MKV_ERR_TIMEOUT);
+                    break;   // the result is lost; what is on its way is waited for at the end
                 }
-                ok = __all_sync(kFull, ok);
-                if (!ok) continue;   // the result is lost; what is on its way is waited for at the end
-                const int tok = (first + i) << 4;
-                const bool edge = first + i >= full_hi || first + i < full_lo;
                 const uint32_t at = ring + stage * C::kStage;
-                if constexpr (KIND == MKV_INT4) {
-                    if (edge) block_int4<D, NT, Q32, HL, true>(st, q, a, u, pos, at, tok, lane);
-                    else block_int4<D, NT, Q32, HL, false>(st, q, a, u, pos, at, tok, lane);
-                } else if constexpr (KIND == MKV_F32) {
-                    const uint32_t weights = ptx::smem_u32(smem) + C::kRing + C::kMerge + C::kMl + warp * 512;
-                    if (edge) block_f32<D, true>(st, q, a, u, pos[0], at, weights, tok, lane);
-                    else block_f32<D, false>(st, q, a, u, pos[0], at, weights, tok, lane);
+                if ((unsigned)(i - full_lo) < (unsigned)full_n) {
+                    if constexpr (KIND == MKV_INT4) block_int4<D, NT, Q32, HL, false>(st, q, a, u, at, 0, lane);
+                    else if constexpr (KIND == MKV_F32) block_f32<D, false>(st, q, a, u, at, weights, 0, lane);
+                    else block_bf16<D, NT, false>(st, q, a, u, at, 0, lane);
                 } else {
-                    if (edge) block_bf16<D, NT, true>(st, q, a, u, pos, at, tok, lane);
-                    else block_bf16<D, NT, false>(st, q, a, u, pos, at, tok, lane);
+                    const int tok = (u.blk0 + (int)(max(u.base, s_range.t0) - u.base) + i) << 4;
+                    if constexpr (KIND == MKV_INT4) block_int4<D, NT, Q32, HL, true>(st, q, a, u, at, tok, lane);
+                    else if constexpr (KIND == MKV_F32) block_f32<D, true>(st, q, a, u, at, weights, tok, lane);
+                    else block_bf16<D, NT, true>(st, q, a, u, at, tok, lane);
                 }
                 __syncwarp();
-                --in_flight;
+                fetch(stage);
                 if (++stage == C::kStages) { stage = 0; parity ^= 1; }
-                fetch();
             }
         }
         if constexpr (KIND == MKV_F32) put_state<D>(st, merge + warp * RT * DP, mls + warp * RT, lane);
@@ -913,12 +912,12 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendAr
         __syncthreads();
     }
     if (tid == 0) leave_join(a, s_range, s_unit);
-    // copies still on their way after a wait that ran out
-    while (in_flight > 0) {
-        paged_wait(bar0 + stage * 8, parity);
-        if (++stage == C::kStages) { stage = 0; parity ^= 1; }
-        --in_flight;
-    }
+    // copies still on their way after a wait that ran out (a stage without one takes its wait's limit)
+    if (!ok)
+        for (int i = 0; i < C::kStages; ++i) {
+            paged_wait(bar0 + stage * 8, parity);
+            if (++stage == C::kStages) { stage = 0; parity ^= 1; }
+        }
 }
 
 template <int KIND, int D, int NT, bool Q32, bool HL>
