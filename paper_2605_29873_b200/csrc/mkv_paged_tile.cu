@@ -6,15 +6,16 @@
 //
 // A CTA is a pipeline over its tiles.  Its 256 rows are two halves of 128, one row per thread of a
 // softmax warpgroup:
-//   MMA thread   S_h = Q_h K^T (shared memory x shared memory -> tensor memory, 128 x 128 fp32), then
-//                O_h += P_h V (tensor memory x shared memory), for the halves in turn: while one half's
-//                products run, the other half's softmax does.
+//   MMA thread   S_h = Q_h K^T (shared memory x shared memory -> tensor memory, 128 x 64 fp32) and
+//                O_h += P_h V (tensor memory x shared memory), for the halves in turn and S one step ahead: every half
+//                has two buffers of S, so that its softmax never waits for a product.  (One buffer of 128 columns,
+//                whose next S has to wait for P V: 4400 cycles for 128 tokens, of which the softmax waited 2000.)
 //   softmax      reads its row of S, p = 2^(s - m), writes P over S as 16-bit.  m is a reference that
 //                moves only when a logit exceeds it by 2^8; O is rescaled then, by the row's own thread.
 //   producer     bf16 pages: bulk tensor copies, 128-byte swizzle.  4-bit pages: a warpgroup turns codes into
 //                fp16 rows (value / 2^f, f by the tile's largest, so that fp16 holds any cache), the
 //                next tile's words already in registers.
-// Tensor memory: S0 S1 O0 O1, 128 columns each.  Shared memory (head_dim 128): Q 64 KB, two stages of K and V
+// Tensor memory: S0 (two buffers), S1, O0, O1, 128 columns each.  Shared memory (head_dim 128): Q 64 KB, two stages of K and V
 // 128 KB.
 // The second product's weights are one bf16 (2^-9 rounding, as the values they multiply have), over 4-bit pages
 // one fp16.  Sums, references and O are fp32; the sum of p is taken before the rounding.
@@ -28,7 +29,7 @@
 namespace mkv {
 namespace {
 
-constexpr int kRows = 256, kTile = 128;
+constexpr int kRows = 256, kTile = 128, kSub = 64;   // rows of a unit; cached tokens of a stage, of a product
 constexpr int kSoft = 256;                  // softmax threads
 constexpr unsigned kFull = 0xffffffffu;
 // Tokens with non-finite values that only some rows of a unit see.  A unit has at most 2 x 255 of them (the
@@ -46,6 +47,11 @@ struct TileCfg {
 };
 
 // ---- tcgen05 and friends
+// Shared-memory operands have 128-byte rows of 64 channels, 128-byte swizzle: groups of 8 rows are 1024 bytes.  The high word of
+// their descriptor; the low word is the address / 16 and, above it, the bytes / 16 to the next 64 channels where the channels
+// are the operand's outer dimension (V).
+constexpr uint32_t kDescHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
+__host__ __device__ constexpr uint32_t desc_lead(uint32_t bytes) { return (bytes >> 4) << 16; }
 __device__ inline void tmem_alloc(uint32_t dst, int cols) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -58,17 +64,23 @@ __device__ inline void fence_after() { asm volatile("tcgen05.fence::after_thread
 __device__ inline void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ inline void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+// D in tensor memory, B (and A) in shared memory: the descriptors' low words, the high word is the same for all
+__device__ inline void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+        "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.u32 p, %4, 0;\n\tmov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(add), "r"(kDescHigh) : "memory");
 }
-__device__ inline void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+__device__ inline void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+        "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.u32 p, %4, 0;\n\tmov.b64 y, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(add), "r"(kDescHigh) : "memory");
+}
+__device__ inline bool one_lane() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
 #define MKV_R8(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
 #define MKV_I8(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
@@ -93,11 +105,6 @@ __device__ inline void tmem_st16(uint32_t addr, const uint32_t (&v)[16]) {
 __device__ inline void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ inline void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Shared-memory operand with 128-byte rows of 64 channels, 128-byte swizzle: groups of 8 rows are 1024 bytes.
-// `lead`: bytes to the next 64 channels where the channels are the operand's outer dimension (V).
-__device__ inline uint64_t smem_desc(uint32_t addr, uint32_t lead) {
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
 // fp32 accumulator, A and B both bf16 (1) or fp16 (0), M = 128, N columns; `b_outer`: B's outer dimension is contiguous
 __host__ __device__ constexpr uint32_t mma_desc(int type, int n, bool b_outer) {
     return 1u << 4 | (uint32_t)type << 7 | (uint32_t)type << 10 | (uint32_t)b_outer << 16 | (uint32_t)(n >> 3) << 17 | (128u >> 4) << 24;
@@ -129,7 +136,7 @@ __device__ inline uint4 lds128(uint32_t addr) {
 __device__ inline uint32_t chunk_at(uint32_t tile, int r, int c) { return tile + (c >> 3) * (128 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
 
 struct Shared {
-    unsigned long long q_full[2], s_full[2], p_full[2], o_full[2];
+    unsigned long long q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2];
     unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2];
     uint32_t tmem;
     int dead;                       // a wait ran out: everybody leaves
@@ -237,23 +244,19 @@ __device__ inline void max32(const uint32_t (&v)[32], float (&mx)[4]) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(v[e + 2 * k]), __uint_as_float(v[e + 2 * k + 1]));
 }
-// Largest visible logit of the row (bottom < column <= top), 32 columns on their way while 32 are looked at.
+// Largest visible logit of the row's 64 (bottom < column <= top).
 template <bool EDGE>
 __device__ inline float row_max(uint32_t sT, int top, int bottom) {
     float mx[4] = {kPagedNegInf, kPagedNegInf, kPagedNegInf, kPagedNegInf};
     uint32_t x[32], y[32];
     tmem_ld32(sT, x);
-#pragma unroll 1
-    for (int c = 0; c < kTile; c += 64) {
-        wait_ld();
-        tmem_ld32(sT + c + 32, y);
-        hide<EDGE>(x, c, top, bottom);
-        max32(x, mx);
-        wait_ld();
-        if (c + 64 < kTile) tmem_ld32(sT + c + 64, x);
-        hide<EDGE>(y, c + 32, top, bottom);
-        max32(y, mx);
-    }
+    wait_ld();
+    tmem_ld32(sT + 32, y);
+    hide<EDGE>(x, 0, top, bottom);
+    max32(x, mx);
+    wait_ld();
+    hide<EDGE>(y, 32, top, bottom);
+    max32(y, mx);
     return fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
 }
 template <int KIND>
@@ -276,17 +279,13 @@ __device__ inline float row_weights(uint32_t sT, float mul, float ref, int top, 
     uint64_t sum[2] = {0, 0};
     uint32_t x[32], y[32];
     tmem_ld32(sT, x);
-#pragma unroll 1
-    for (int c = 0; c < kTile; c += 64) {
-        wait_ld();
-        tmem_ld32(sT + c + 32, y);
-        hide<EDGE>(x, c, top, bottom);
-        weights32<KIND>(x, sT + c / 2, m2, r2, sum);
-        wait_ld();
-        if (c + 64 < kTile) tmem_ld32(sT + c + 64, x);
-        hide<EDGE>(y, c + 32, top, bottom);
-        weights32<KIND>(y, sT + c / 2 + 16, m2, r2, sum);
-    }
+    wait_ld();
+    tmem_ld32(sT + 32, y);
+    hide<EDGE>(x, 0, top, bottom);
+    weights32<KIND>(x, sT, m2, r2, sum);
+    wait_ld();
+    hide<EDGE>(y, 32, top, bottom);
+    weights32<KIND>(y, sT + 16, m2, r2, sum);
     const float2 s = unpair(add2(sum[0], sum[1]));
     return s.x + s.y;
 }
@@ -298,12 +297,14 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
     const int tid = threadIdx.x, w = tid >> 7, row = tid & 127, warp4 = (tid >> 5) & 3, lane = tid & 31;
     const int warp_row = (tid >> 5) * 32;   // first row of the warp, of the unit's 256
     const uint32_t lanes = (uint32_t)(warp4 * 32) << 16;
-    const uint32_t sT = sh.tmem + lanes + w * 128, oT = sh.tmem + lanes + 256 + w * 128;
-    const uint32_t q_full = ptx::smem_u32(&sh.q_full[w]), s_full = ptx::smem_u32(&sh.s_full[w]), p_full = ptx::smem_u32(&sh.p_full[w]),
-                   o_full = ptx::smem_u32(&sh.o_full[w]);
+    const uint32_t sT = sh.tmem + lanes + w * 128, oT = sh.tmem + lanes + 256 + w * 128;   // two buffers of 64 columns for S
+    const uint32_t q_full = ptx::smem_u32(&sh.q_full[w]), p_full = ptx::smem_u32(&sh.p_full[w][0]);   // one for each buffer: a warp may be a step ahead of another
+    // Of the products P V two barriers tell, in turn: a wait cannot miss more than the one before, and S of a step says that
+    // all up to two steps before are done.
+    auto pv_done = [&](uint32_t i) { return ptx::smem_u32(&sh.pv_done[w][i & 1]); };
     const RowsOut rows_out{smem + C::kOut + (tid >> 5) * 8192, lane};
     const uint32_t q_smem = smem + w * C::kHalf, v_smem = smem + 4 * C::kHalf;
-    uint32_t s_par = 0, o_par = 0;
+    uint32_t subs = 0;        // products of this half so far: parity of S and O
     int tiles = 0;            // of this CTA so far: stage and parity of K and V
     Unit u = sh.unit;
     for (;;) {
@@ -414,47 +415,53 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                         ptx::fence_proxy_async();
                     }
                 }
-                if (!(ok = __all_sync(kFull, wait_or_leave(a, sh, s_full, s_par)))) break;
-                s_par ^= 1;
-                fence_after();
                 float mul = back, f = 0.f;
                 if (KIND == MKV_INT4) {
                     if (!(ok = __all_sync(kFull, wait_or_leave(a, sh, ptx::smem_u32(&sh.v_full[stage]), par)))) break;
                     mul *= sh.k_mul[stage];
                     f = sh.v_exp[stage];
                 }
-                const int top = place.pos - t0, bottom = a.window > 0 ? top - a.window : INT_MIN;   // bottom < column <= top
-                float mx = edge ? row_max<true>(sT, top, bottom) : row_max<false>(sT, 0, 0);
-                mx = fmaf(mx, mul, f);
-                const bool move = mx > m + 8.f;
-                if (__any_sync(kFull, move)) {
-                    const float mn = move ? mx : m, sc = ex2(m - mn);
-                    m = mn;
-                    l *= sc;
-                    if (j > 0) {   // the products before are complete: this tile's S was issued behind them
 #pragma unroll 1
-                        for (int c = 0; c < D / 32; ++c) {
-                            uint32_t v[32];
-                            tmem_ld32(oT + 32 * c, v);
-                            wait_ld();
+                for (int h = 0; h < 2; ++h, ++subs) {
+                    const int t1 = t0 + h * kSub;
+                    if (!(ok = __all_sync(kFull, wait_or_leave(a, sh, ptx::smem_u32(&sh.s_full[w][h]), (subs >> 1) & 1)))) break;
+                    fence_after();
+                    const bool cut = t1 + kSub - 1 > u.plo || (a.window > 0 && t1 <= u.phi - a.window);
+                    const int top = place.pos - t1, bottom = a.window > 0 ? top - a.window : INT_MIN;   // bottom < column <= top
+                    const uint32_t sH = sT + h * kSub;
+                    float mx = cut ? row_max<true>(sH, top, bottom) : row_max<false>(sH, 0, 0);
+                    mx = fmaf(mx, mul, f);
+                    const bool move = mx > m + 8.f;
+                    if (__any_sync(kFull, move)) {
+                        const float mn = move ? mx : m, sc = ex2(m - mn);
+                        m = mn;
+                        l *= sc;
+                        if (j + h > 0) {   // O is complete up to the product before
+                            if (!(ok = __all_sync(kFull, wait_or_leave(a, sh, pv_done(subs - 1), ((subs - 1) >> 1) & 1)))) break;
+                            fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < D / 32; ++c) {
+                                uint32_t v[32];
+                                tmem_ld32(oT + 32 * c, v);
+                                wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * sc);
-                            tmem_st32(oT + 32 * c, v);
+                                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * sc);
+                                tmem_st32(oT + 32 * c, v);
+                            }
                         }
-                        wait_st();
                     }
+                    const float ref = f - m;
+                    const float sum = cut ? row_weights<KIND, true>(sH, mul, ref, top, bottom) : row_weights<KIND, false>(sH, mul, ref, 0, 0);
+                    l += KIND == MKV_INT4 ? sum * ex2(-f) : sum;
+                    wait_st();
+                    fence_before();
+                    ptx::mbar_arrive(p_full + 8 * h);
                 }
-                const float ref = f - m;
-                const float sum = edge ? row_weights<KIND, true>(sT, mul, ref, top, bottom) : row_weights<KIND, false>(sT, mul, ref, 0, 0);
-                l += KIND == MKV_INT4 ? sum * ex2(-f) : sum;
-                wait_st();
-                fence_before();
-                ptx::mbar_arrive(p_full);
+                if (!ok) break;
             }
         }
         if (active && nt > 0 && ok) {
-            ok = wait_or_leave(a, sh, o_full, o_par);
-            o_par ^= 1;
+            ok = wait_or_leave(a, sh, pv_done(subs - 1), ((subs - 1) >> 1) & 1);
             fence_after();
         }
         if (any_leaves(!ok)) {   // and the list of odd tokens is complete
@@ -515,66 +522,84 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
     }
 }
 
-// ---- the MMA thread
+// ---- the MMA warp
 template <int KIND, int D>
 __device__ inline void mma_role(const PagedAttendArgs& a, Shared& sh, const Range& rg, uint32_t smem) {
     using C = TileCfg<D>;
     constexpr int kType = KIND == MKV_BF16 ? 1 : 0;
-    constexpr uint32_t qk = mma_desc(kType, kTile, false), pv = mma_desc(kType, D, true);
+    constexpr uint32_t qk = mma_desc(kType, kSub, false), pv = mma_desc(kType, D, true);
     auto bar = [](unsigned long long& b) { return ptx::smem_u32(&b); };
     uint32_t q_par = 0, q1_par = 0, p_par[2] = {0, 0};
     int tiles = 0;
     Unit u = sh.unit;
-    auto qk_product = [&](int w, int stage) {
+    // The whole warp is here, so that addresses stay in uniform registers; one lane issues.
+    const uint32_t tmem = sh.tmem;
+    const uint32_t q_lo = (smem >> 4) | desc_lead(16), k_lo = ((smem + 2 * C::kHalf) >> 4) | desc_lead(16),
+                   v_lo = ((smem + 4 * C::kHalf) >> 4) | desc_lead(128 * 128);
+    // S of half w, tokens 64 h .. of the stage, into its buffer h
+    auto qk_product = [&](int w, int stage, int h) {
+        if (one_lane()) {
+            const uint32_t a0 = q_lo + w * (C::kHalf >> 4), b0 = k_lo + stage * (C::kHalf >> 4) + h * (kSub * 128 >> 4), d = tmem + w * 128 + h * kSub;
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            const uint32_t off = (k >> 2) * (128 * 128) + (k & 3) * 32;
-            mma_ss(sh.tmem + w * 128, smem_desc(smem + w * C::kHalf + off, 16), smem_desc(smem + (2 + stage) * C::kHalf + off, 16), qk, k > 0);
+            for (int k = 0; k < D / 16; ++k) {
+                constexpr uint32_t kChunk = 128 * 128 >> 4;
+                mma_ss(d, a0 + (k >> 2) * kChunk + (k & 3) * 2, b0 + (k >> 2) * kChunk + (k & 3) * 2, qk, k > 0);
+            }
+            mma_commit(bar(sh.s_full[w][h]));
         }
+        __syncwarp();
     };
-    auto pv_product = [&](int w, int stage, bool add) {
+    auto pv_product = [&](int w, int stage, int h, bool add) {
+        if (one_lane()) {
+            const uint32_t d = tmem + 256 + w * 128, a0 = tmem + w * 128 + h * kSub, b0 = v_lo + stage * (C::kHalf >> 4) + h * (kSub * 128 >> 4);
 #pragma unroll
-        for (int k = 0; k < kTile / 16; ++k)
-            mma_ts(sh.tmem + 256 + w * 128, sh.tmem + w * 128 + 8 * k, smem_desc(smem + (4 + stage) * C::kHalf + k * 2048, 128 * 128), pv, add || k > 0);
+            for (int k = 0; k < kSub / 16; ++k) mma_ts(d, a0 + 8 * k, b0 + k * (2048 >> 4), pv, add || k > 0);
+            mma_commit(bar(sh.pv_done[w][h]));
+        }
+        __syncwarp();
     };
+    auto commit = [&](unsigned long long& b) {
+        if (one_lane()) mma_commit(bar(b));
+        __syncwarp();
+    };
+    auto ready = [&](uint32_t b, uint32_t par) { return __all_sync(kFull, wait_or_leave(a, sh, b, par)); };
     for (;;) {
         const long long lo = max(u.base, rg.t0), hi = min(u.end(), rg.t1);
         const int nt = u.nblk == 0 ? 0 : (int)(hi - lo);
         const int halves = u.rows > 128 ? 2 : 1;
         if (nt > 0) {
-            if (!wait_or_leave(a, sh, bar(sh.q_full[0]), q_par)) return;
+            if (!ready(bar(sh.q_full[0]), q_par)) return;
             q_par ^= 1;
             if (halves == 2) {
-                if (!wait_or_leave(a, sh, bar(sh.q_full[1]), q1_par)) return;
+                if (!ready(bar(sh.q_full[1]), q1_par)) return;
                 q1_par ^= 1;
             }
-            if (!wait_or_leave(a, sh, bar(sh.k_full[tiles & 1]), (tiles >> 1) & 1)) return;
+            if (!ready(bar(sh.k_full[tiles & 1]), (tiles >> 1) & 1)) return;
             fence_after();
-            for (int w = 0; w < halves; ++w) {
-                qk_product(w, tiles & 1);
-                mma_commit(bar(sh.s_full[w]));
-            }
-            mma_commit(bar(sh.k_empty[tiles & 1]));
+            for (int w = 0; w < halves; ++w) qk_product(w, tiles & 1, 0);
         }
+        // Every S is issued one product ahead of the P that its row's threads are at: when they are done with one, the next
+        // is there.  (A buffer's new S is issued behind the product that read its old P: the unit runs them in order.)
+#pragma unroll 1
         for (int j = 0; j < nt; ++j) {
             const int t = tiles + j, stage = t & 1, next = (t + 1) & 1;
             const bool more = j + 1 < nt;
-            if (!wait_or_leave(a, sh, bar(sh.v_full[stage]), (t >> 1) & 1)) return;
-            if (more && !wait_or_leave(a, sh, bar(sh.k_full[next]), ((t + 1) >> 1) & 1)) return;
-            for (int w = 0; w < halves; ++w) {
-                if (!wait_or_leave(a, sh, bar(sh.p_full[w]), p_par[w])) return;
-                p_par[w] ^= 1;
+            if (!ready(bar(sh.v_full[stage]), (t >> 1) & 1)) return;
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                if (h == 1 && more && !ready(bar(sh.k_full[next]), ((t + 1) >> 1) & 1)) return;
                 fence_after();
-                pv_product(w, stage, j > 0);
-                if (w == halves - 1) mma_commit(bar(sh.v_empty[stage]));
-                if (more) {
-                    qk_product(w, next);
-                    mma_commit(bar(sh.s_full[w]));
-                } else {
-                    mma_commit(bar(sh.o_full[w]));
+                for (int w = 0; w < halves; ++w) {
+                    if (h == 0) qk_product(w, stage, 1);
+                    else if (more) qk_product(w, next, 0);
+                    if (h == 0 && w == halves - 1) commit(sh.k_empty[stage]);
+                    if (!ready(bar(sh.p_full[w][h]), p_par[w])) return;
+                    if (h == 1) p_par[w] ^= 1;
+                    fence_after();
+                    pv_product(w, stage, h, j + h > 0);
                 }
             }
-            if (more) mma_commit(bar(sh.k_empty[next]));
+            commit(sh.v_empty[stage]);
         }
         tiles += nt;
         if (u.end() >= rg.t1 || !next_unit<kRows, kTile>(a, u)) return;
@@ -632,15 +657,16 @@ struct RawTile {
     uint32_t ks[NG], kl[NG / 2], vs[NG], vl[NG];
 };
 
-template <int D>
+template <int D, bool K, bool V>
 __device__ inline void load_raw(const PagedAttendArgs& a, const Unit& u, int t0, int id, RawTile<D>& x) {
     constexpr int NG = D / 32;
     // K: token t0 + id.  V: pair of tokens t0 + 2 (id / 2), its lower or upper half of the words
     const int p = t0 + id;
 #pragma unroll
-    for (int i = 0; i < NG; ++i) { x.k[i] = x.v[i] = make_uint4(0, 0, 0, 0); x.ks[i] = x.vs[i] = x.vl[i] = 0; }
-#pragma unroll
-    for (int i = 0; i < NG / 2; ++i) x.kl[i] = 0;
+    for (int i = 0; i < NG; ++i) {
+        if (K) { x.k[i] = make_uint4(0, 0, 0, 0); x.ks[i] = 0; x.kl[i / 2] = 0; }
+        if (V) { x.v[i] = make_uint4(0, 0, 0, 0); x.vs[i] = x.vl[i] = 0; }
+    }
     if ((p & ~15) > u.phi) return;
     const uint8_t* head = a.c.pages + (size_t)paged_page(a.c, a.b, u.s, p & ~15) * a.c.page_bytes + (size_t)u.h * a.c.head_bytes;
     const int row = p & ((1 << a.c.page_shift) - 1), r = row & 15;
@@ -648,16 +674,20 @@ __device__ inline void load_raw(const PagedAttendArgs& a, const Unit& u, int t0,
     const uint4* kp = reinterpret_cast<const uint4*>(blk + r * (D / 2));
     const uint4* vp = reinterpret_cast<const uint4*>(blk + 8 * D + (r >> 1) * D + (r & 1) * (D / 2));
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) { x.k[i] = __ldg(kp + i); x.v[i] = __ldg(vp + i); }
+    for (int i = 0; i < D / 32; ++i) {
+        if (K) x.k[i] = __ldg(kp + i);
+        if (V) x.v[i] = __ldg(vp + i);
+    }
     const uint32_t* par = reinterpret_cast<const uint32_t*>(blk + 16 * D);
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
-        x.ks[j] = __ldg(par + (r >> 1) * NG + j);
-        x.vs[j] = __ldg(par + 16 * NG + (r >> 1) * NG + j);
-        x.vl[j] = __ldg(par + 24 * NG + (r >> 1) * NG + j);
+        if (K) x.ks[j] = __ldg(par + (r >> 1) * NG + j);
+        if (V) x.vs[j] = __ldg(par + 16 * NG + (r >> 1) * NG + j);
+        if (V) x.vl[j] = __ldg(par + 24 * NG + (r >> 1) * NG + j);
     }
 #pragma unroll
-    for (int j = 0; j < NG / 2; ++j) x.kl[j] = __ldg(par + 8 * NG + r * (NG / 2) + j);
+    for (int j = 0; j < NG / 2; ++j)
+        if (K) x.kl[j] = __ldg(par + 8 * NG + r * (NG / 2) + j);
 }
 
 __device__ inline __half2 codes_low(uint32_t w) {    // nibbles 0 and 4 as numbers
@@ -707,7 +737,7 @@ __device__ inline void dequant_role(const PagedAttendArgs& a, Shared& sh, const 
             const int stage = tiles & 1;
             const uint32_t par = ((tiles >> 1) & 1) ^ 1;
             const int t0 = (first + j) * kTile;
-            if (fresh) { load_raw<D>(a, u, t0, id, x); fresh = false; }
+            if (fresh) { load_raw<D, true, true>(a, u, t0, id, x); fresh = false; }
             const int begin = a.window > 0 ? max(0, u.plo - a.window + 1) : 0;
             const int p = t0 + id;
             const bool seen = p <= u.phi && p >= begin, other = (p ^ 1) <= u.phi && (p ^ 1) >= begin;
@@ -741,6 +771,7 @@ __device__ inline void dequant_role(const PagedAttendArgs& a, Shared& sh, const 
             }
             ptx::fence_proxy_async();
             ptx::mbar_arrive(ptx::smem_u32(&sh.k_full[stage]));
+            if (j + 1 < nt) load_raw<D, true, false>(a, u, t0 + kTile, id, x);
             // ---- V: tokens id & ~1 and its neighbour, words of g 0..3 or 4..7
             const bool even_seen = id & 1 ? other : seen, odd_seen = id & 1 ? seen : other;
             float vtop = 0.f, s0[NG], l0[NG], s1[NG], l1[NG];
@@ -786,7 +817,7 @@ __device__ inline void dequant_role(const PagedAttendArgs& a, Shared& sh, const 
             }
             ptx::fence_proxy_async();
             ptx::mbar_arrive(ptx::smem_u32(&sh.v_full[stage]));
-            if (j + 1 < nt) load_raw<D>(a, u, t0 + kTile, id, x);
+            if (j + 1 < nt) load_raw<D, false, true>(a, u, t0 + kTile, id, x);
         }
         if (u.end() >= rg.t1 || !next_unit<kRows, kTile>(a, u)) return;
         part_of(u, first, nt);
@@ -818,7 +849,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendArgs
     if (tid == 0) {
         auto init = [](unsigned long long& b, int n) { ptx::mbar_init(ptx::smem_u32(&b), n); };
         for (int i = 0; i < 2; ++i) {
-            init(sh.q_full[i], 128); init(sh.s_full[i], 1); init(sh.p_full[i], 128); init(sh.o_full[i], 1);
+            init(sh.q_full[i], 128); init(sh.s_full[i][0], 1); init(sh.s_full[i][1], 1); init(sh.p_full[i][0], 128); init(sh.p_full[i][1], 128); init(sh.pv_done[i][0], 1); init(sh.pv_done[i][1], 1);
             init(sh.k_full[i], KIND == MKV_INT4 ? 128 : 1); init(sh.v_full[i], KIND == MKV_INT4 ? 128 : 1);
             init(sh.k_empty[i], 1); init(sh.v_empty[i], 1);
         }
@@ -834,10 +865,10 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendArgs
         softmax_role<KIND, D, IO32>(a, sh, rg, smem);
     } else if (KIND == MKV_INT4) {
         if (tid < kSoft + 128) dequant_role<D>(a, sh, rg, smem, tid - kSoft);
-        else if (tid == kSoft + 128) mma_role<KIND, D>(a, sh, rg, smem);
+        else mma_role<KIND, D>(a, sh, rg, smem);
     } else {
         if (tid == kSoft) copy_role<D>(a, sh, rg, smem, &map, layer_rows);
-        else if (tid == kSoft + 32) mma_role<KIND, D>(a, sh, rg, smem);
+        else if (tid >= kSoft + 32) mma_role<KIND, D>(a, sh, rg, smem);
     }
     __syncwarp();
     fence_before();
