@@ -6,16 +6,18 @@
 //
 // A CTA is a pipeline over its tiles.  Its 256 rows are two halves of 128, one row per thread of a
 // softmax warpgroup:
-//   MMA thread   S_h = Q_h K^T (shared memory x shared memory -> tensor memory, 128 x 64 fp32) and
-//                O_h += P_h V (tensor memory x shared memory), for the halves in turn and S one step ahead: every half
-//                has two buffers of S, so that its softmax never waits for a product.  (One buffer of 128 columns,
-//                whose next S has to wait for P V: 4400 cycles for 128 tokens, of which the softmax waited 2000.)
+//   MMA warp     S_h = Q_h K^T (shared memory x shared memory -> tensor memory, 128 x 128 fp32), then
+//                O_h += P_h V (tensor memory x shared memory, in two steps of 64 tokens, the first while the weights of the
+//                others are still being made), for the halves in turn: while one half's products run, the other half's
+//                softmax does.
+//                (Two buffers of 64 columns for S, with S a step ahead, were no faster: a 128 x 64 product takes the same 70
+//                cycles as a 128 x 128 one, for both read 128 rows of Q.)
 //   softmax      reads its row of S, p = 2^(s - m), writes P over S as 16-bit.  m is a reference that
 //                moves only when a logit exceeds it by 2^8; O is rescaled then, by the row's own thread.
 //   producer     bf16 pages: bulk tensor copies, 128-byte swizzle.  4-bit pages: a warpgroup turns codes into
 //                fp16 rows (value / 2^f, f by the tile's largest, so that fp16 holds any cache), the
 //                next tile's words already in registers.
-// Tensor memory: S0 (two buffers), S1, O0, O1, 128 columns each.  Shared memory (head_dim 128): Q 64 KB, two stages of K and V
+// Tensor memory: S0 S1 O0 O1, 128 columns each.  Shared memory (head_dim 128): Q 64 KB, two stages of K and V
 // 128 KB.
 // The second product's weights are one bf16 (2^-9 rounding, as the values they multiply have), over 4-bit pages
 // one fp16.  Sums, references and O are fp32; the sum of p is taken before the rounding.
@@ -29,14 +31,15 @@
 namespace mkv {
 namespace {
 
-constexpr int kRows = 256, kTile = 128, kSub = 64;   // rows of a unit; cached tokens of a stage, of a product
+constexpr int kRows = 256, kTile = 128;     // rows of a unit, cached tokens of a tile
 constexpr int kSoft = 256;                  // softmax threads
 constexpr unsigned kFull = 0xffffffffu;
 // Tokens with non-finite values that only some rows of a unit see.  A unit has at most 2 x 255 of them (the
 // diagonal and the window's edge), and the producers are at most three units ahead.
 constexpr int kOddMax = 2048;
 
-template <int KIND> __host__ __device__ constexpr int threads_of() { return kSoft + (KIND == MKV_INT4 ? 128 + 32 : 64); }
+// 4 bits: two warpgroups of softmax, one that turns codes into rows, one for the MMA warp; registers are dealt out by need
+template <int KIND> __host__ __device__ constexpr int threads_of() { return kSoft + (KIND == MKV_INT4 ? 256 : 128); }
 
 template <int D>
 struct TileCfg {
@@ -91,11 +94,10 @@ __device__ inline void tmem_ld32(uint32_t addr, uint32_t (&v)[32]) {
         "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
         : MKV_R8(v, 0), MKV_R8(v, 8), MKV_R8(v, 16), MKV_R8(v, 24) : "r"(addr));
 }
-__device__ inline void tmem_st32(uint32_t addr, const uint32_t (&v)[32]) {
+__device__ inline void tmem_ld16(uint32_t addr, uint32_t (&v)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
-        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
-        ::MKV_I8(v, 0), MKV_I8(v, 8), MKV_I8(v, 16), MKV_I8(v, 24), "r"(addr) : "memory");
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : MKV_R8(v, 0), MKV_R8(v, 8) : "r"(addr));
 }
 __device__ inline void tmem_st16(uint32_t addr, const uint32_t (&v)[16]) {
     asm volatile(
@@ -136,7 +138,7 @@ __device__ inline uint4 lds128(uint32_t addr) {
 __device__ inline uint32_t chunk_at(uint32_t tile, int r, int c) { return tile + (c >> 3) * (128 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
 
 struct Shared {
-    unsigned long long q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2];
+    unsigned long long q_full[2], s_full[2], p_full[2][2], o_full[2];
     unsigned long long k_full[2], k_empty[2], v_full[2], v_empty[2];
     uint32_t tmem;
     int dead;                       // a wait ran out: everybody leaves
@@ -150,10 +152,17 @@ struct Shared {
 
 // Waits that end: false once any of the CTA's waits ran out.
 __device__ inline bool wait_or_leave(const PagedAttendArgs& a, Shared& sh, uint32_t bar, uint32_t parity) {
-    if (*(volatile int*)&sh.dead) return false;
-    if (paged_wait(bar, parity)) return true;
-    *(volatile int*)&sh.dead = 1;
-    paged_fail(a.c, MKV_ERR_TIMEOUT);
+    for (int i = 0; i < 8; ++i)
+        if (ptx::mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (!*(volatile int*)&sh.dead) {
+        for (int i = 0; i < 32; ++i)
+            if (ptx::mbar_try_wait(bar, parity)) return true;
+        if (clock64() - t0 > (1ll << 32)) {
+            *(volatile int*)&sh.dead = 1;
+            paged_fail(a.c, MKV_ERR_TIMEOUT);
+        }
+    }
     return false;
 }
 
@@ -231,62 +240,80 @@ __device__ inline float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
     return y;
 }
+// The row's 128 logits, and the largest visible one of them (bottom < column <= top); others become -inf.
 template <bool EDGE>
-__device__ inline void hide(uint32_t (&v)[32], int c, int top, int bottom) {
-    if (!EDGE) return;
+__device__ inline float row_logits(uint32_t sT, int top, int bottom, uint32_t (&x)[4][32]) {
 #pragma unroll
-    for (int e = 0; e < 32; ++e)
-        if (c + e > top || c + e <= bottom) v[e] = 0xff800000u;
-}
-__device__ inline void max32(const uint32_t (&v)[32], float (&mx)[4]) {
-#pragma unroll
-    for (int e = 0; e < 32; e += 8)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(v[e + 2 * k]), __uint_as_float(v[e + 2 * k + 1]));
-}
-// Largest visible logit of the row's 64 (bottom < column <= top).
-template <bool EDGE>
-__device__ inline float row_max(uint32_t sT, int top, int bottom) {
+    for (int c = 0; c < 4; ++c) tmem_ld32(sT + 32 * c, x[c]);
+    wait_ld();
     float mx[4] = {kPagedNegInf, kPagedNegInf, kPagedNegInf, kPagedNegInf};
-    uint32_t x[32], y[32];
-    tmem_ld32(sT, x);
-    wait_ld();
-    tmem_ld32(sT + 32, y);
-    hide<EDGE>(x, 0, top, bottom);
-    max32(x, mx);
-    wait_ld();
-    hide<EDGE>(y, 32, top, bottom);
-    max32(y, mx);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+            if (EDGE && (32 * c + e > top || 32 * c + e <= bottom)) x[c][e] = 0xff800000u;
+#pragma unroll
+        for (int e = 0; e < 32; e += 8)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(x[c][e + 2 * k]), __uint_as_float(x[c][e + 2 * k + 1]));
+    }
     return fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
 }
-template <int KIND>
+
+// 2^x of a pair on the fused multiply-add units, for part of the elements: the special-function unit's four a clock would
+// bound the kernel.  x in [-126, 126] (less counts as -126; a NaN stays one): n = rint(x) in the low bits of
+// x + 1.5 * 2^23 + 127, where it is the exponent field of 2^n already, times a polynomial in x - n, |x - n| <= 1/2, fitted for
+// the least relative error (1.6e-7).
+__device__ inline uint64_t ex2_poly(uint64_t x) {
+    float2 v = unpair(x);
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(v.x) : "f"(v.x), "f"(-126.f));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(v.y) : "f"(v.y), "f"(-126.f));
+    x = pair(v.x, v.y);
+    constexpr float kBias = 12582912.f + 127.f;
+    const uint64_t t = add2(x, pair(kBias, kBias));
+    const uint64_t f = add2(x, fma2(t, pair(-1.f, -1.f), pair(kBias, kBias)));
+    uint64_t p = pair(0.0013276468962430954f, 0.0013276468962430954f);
+    p = fma2(p, f, pair(0.009675540961325169f, 0.009675540961325169f));
+    p = fma2(p, f, pair(0.05550713464617729f, 0.05550713464617729f));
+    p = fma2(p, f, pair(0.24022120237350464f, 0.24022120237350464f));
+    p = fma2(p, f, pair(0.6931469440460205f, 0.6931469440460205f));
+    p = fma2(p, f, pair(1.f, 1.f));
+    const float2 n = unpair(t);
+    return mul2(p, pair(__uint_as_float(__float_as_uint(n.x) << 23), __uint_as_float(__float_as_uint(n.y) << 23)));
+}
+
+template <int KIND, bool EDGE>
 __device__ inline void weights32(const uint32_t (&v)[32], uint32_t pT, uint64_t mul, uint64_t ref, uint64_t (&sum)[2]) {
     uint32_t pk[16];
 #pragma unroll
-    for (int e = 0; e < 32; e += 2) {
-        const float2 x = unpair(fma2(pair(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), mul, ref));
-        const float p0 = ex2(x.x), p1 = ex2(x.y);
-        sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pair(p0, p1));
-        pk[e >> 1] = KIND == MKV_BF16 ? ptx::pack_bf16x2(p0, p1) : pack_f16x2(p0, p1);
+    for (int i = 0; i < 16; ++i) {
+        const uint64_t x = fma2(pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), mul, ref);
+        // three pairs of eight (of sixteen beside the threads that turn codes into rows); not where -inf has to give 0
+        const bool poly = !EDGE && (KIND == MKV_BF16 ? (i & 7) == 1 || (i & 7) == 4 || (i & 7) == 6 : (i & 7) == 1 || i == 4);
+        uint64_t p;
+        if (poly) {
+            p = ex2_poly(x);
+        } else {
+            const float2 y = unpair(x);
+            p = pair(ex2(y.x), ex2(y.y));
+        }
+        sum[i & 1] = add2(sum[i & 1], p);
+        const float2 y = unpair(p);
+        pk[i] = KIND == MKV_BF16 ? ptx::pack_bf16x2(y.x, y.y) : pack_f16x2(y.x, y.y);
     }
     tmem_st16(pT, pk);
 }
-// The row's weights 2^(s * mul + ref), over S in tensor memory; returns their sum.  The 16-bit weights of columns
-// c.. go to columns c / 2.., behind what is still to be read.
+// Weights 2^(s * mul + ref) of 64 columns, 16 bits each, into tensor memory (over S, which has been read); returns their sum
+// once they are there.
 template <int KIND, bool EDGE>
-__device__ inline float row_weights(uint32_t sT, float mul, float ref, int top, int bottom) {
+__device__ inline float row_weights(const uint32_t (&x)[32], const uint32_t (&y)[32], uint32_t pT, float mul, float ref) {
     const uint64_t m2 = pair(mul, mul), r2 = pair(ref, ref);
     uint64_t sum[2] = {0, 0};
-    uint32_t x[32], y[32];
-    tmem_ld32(sT, x);
-    wait_ld();
-    tmem_ld32(sT + 32, y);
-    hide<EDGE>(x, 0, top, bottom);
-    weights32<KIND>(x, sT, m2, r2, sum);
-    wait_ld();
-    hide<EDGE>(y, 32, top, bottom);
-    weights32<KIND>(y, sT + 16, m2, r2, sum);
+    weights32<KIND, EDGE>(x, pT, m2, r2, sum);
+    weights32<KIND, EDGE>(y, pT + 16, m2, r2, sum);
     const float2 s = unpair(add2(sum[0], sum[1]));
+    wait_st();
+    fence_before();
     return s.x + s.y;
 }
 
@@ -297,14 +324,12 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
     const int tid = threadIdx.x, w = tid >> 7, row = tid & 127, warp4 = (tid >> 5) & 3, lane = tid & 31;
     const int warp_row = (tid >> 5) * 32;   // first row of the warp, of the unit's 256
     const uint32_t lanes = (uint32_t)(warp4 * 32) << 16;
-    const uint32_t sT = sh.tmem + lanes + w * 128, oT = sh.tmem + lanes + 256 + w * 128;   // two buffers of 64 columns for S
-    const uint32_t q_full = ptx::smem_u32(&sh.q_full[w]), p_full = ptx::smem_u32(&sh.p_full[w][0]);   // one for each buffer: a warp may be a step ahead of another
-    // Of the products P V two barriers tell, in turn: a wait cannot miss more than the one before, and S of a step says that
-    // all up to two steps before are done.
-    auto pv_done = [&](uint32_t i) { return ptx::smem_u32(&sh.pv_done[w][i & 1]); };
+    const uint32_t sT = sh.tmem + lanes + w * 128, oT = sh.tmem + lanes + 256 + w * 128;
+    const uint32_t q_full = ptx::smem_u32(&sh.q_full[w]), p_full = ptx::smem_u32(&sh.p_full[w][0]);   // two: the first 64 columns, the others
+    const uint32_t s_full = ptx::smem_u32(&sh.s_full[w]), o_full = ptx::smem_u32(&sh.o_full[w]);
     const RowsOut rows_out{smem + C::kOut + (tid >> 5) * 8192, lane};
     const uint32_t q_smem = smem + w * C::kHalf, v_smem = smem + 4 * C::kHalf;
-    uint32_t subs = 0;        // products of this half so far: parity of S and O
+    uint32_t s_par = 0, o_par = 0;
     int tiles = 0;            // of this CTA so far: stage and parity of K and V
     Unit u = sh.unit;
     for (;;) {
@@ -421,47 +446,41 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                     mul *= sh.k_mul[stage];
                     f = sh.v_exp[stage];
                 }
+                if (!(ok = __all_sync(kFull, wait_or_leave(a, sh, s_full, s_par)))) break;
+                s_par ^= 1;
+                fence_after();
+                const int top = place.pos - t0, bottom = a.window > 0 ? top - a.window : INT_MIN;   // bottom < column <= top
+                uint32_t x[4][32];
+                float mx = edge ? row_logits<true>(sT, top, bottom, x) : row_logits<false>(sT, 0, 0, x);
+                mx = fmaf(mx, mul, f);
+                const bool move = mx > m + 8.f;
+                if (__any_sync(kFull, move)) {
+                    const float mn = move ? mx : m, sc = ex2(m - mn);
+                    m = mn;
+                    l *= sc;
+                    if (j > 0) {   // O is complete up to the tile before: this tile's S was issued behind its products
 #pragma unroll 1
-                for (int h = 0; h < 2; ++h, ++subs) {
-                    const int t1 = t0 + h * kSub;
-                    if (!(ok = __all_sync(kFull, wait_or_leave(a, sh, ptx::smem_u32(&sh.s_full[w][h]), (subs >> 1) & 1)))) break;
-                    fence_after();
-                    const bool cut = t1 + kSub - 1 > u.plo || (a.window > 0 && t1 <= u.phi - a.window);
-                    const int top = place.pos - t1, bottom = a.window > 0 ? top - a.window : INT_MIN;   // bottom < column <= top
-                    const uint32_t sH = sT + h * kSub;
-                    float mx = cut ? row_max<true>(sH, top, bottom) : row_max<false>(sH, 0, 0);
-                    mx = fmaf(mx, mul, f);
-                    const bool move = mx > m + 8.f;
-                    if (__any_sync(kFull, move)) {
-                        const float mn = move ? mx : m, sc = ex2(m - mn);
-                        m = mn;
-                        l *= sc;
-                        if (j + h > 0) {   // O is complete up to the product before
-                            if (!(ok = __all_sync(kFull, wait_or_leave(a, sh, pv_done(subs - 1), ((subs - 1) >> 1) & 1)))) break;
-                            fence_after();
-#pragma unroll 1
-                            for (int c = 0; c < D / 32; ++c) {
-                                uint32_t v[32];
-                                tmem_ld32(oT + 32 * c, v);
-                                wait_ld();
+                        for (int c = 0; c < D / 16; ++c) {
+                            uint32_t v[16];
+                            tmem_ld16(oT + 16 * c, v);
+                            wait_ld();
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * sc);
-                                tmem_st32(oT + 32 * c, v);
-                            }
+                            for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * sc);
+                            tmem_st16(oT + 16 * c, v);
                         }
                     }
-                    const float ref = f - m;
-                    const float sum = cut ? row_weights<KIND, true>(sH, mul, ref, top, bottom) : row_weights<KIND, false>(sH, mul, ref, 0, 0);
-                    l += KIND == MKV_INT4 ? sum * ex2(-f) : sum;
-                    wait_st();
-                    fence_before();
-                    ptx::mbar_arrive(p_full + 8 * h);
                 }
-                if (!ok) break;
+                const float ref = f - m;
+                float sum = edge ? row_weights<KIND, true>(x[0], x[1], sT, mul, ref) : row_weights<KIND, false>(x[0], x[1], sT, mul, ref);
+                ptx::mbar_arrive(p_full);
+                sum += edge ? row_weights<KIND, true>(x[2], x[3], sT + 32, mul, ref) : row_weights<KIND, false>(x[2], x[3], sT + 32, mul, ref);
+                ptx::mbar_arrive(p_full + 8);
+                l += KIND == MKV_INT4 ? sum * ex2(-f) : sum;
             }
         }
         if (active && nt > 0 && ok) {
-            ok = wait_or_leave(a, sh, pv_done(subs - 1), ((subs - 1) >> 1) & 1);
+            ok = wait_or_leave(a, sh, o_full, o_par);
+            o_par ^= 1;
             fence_after();
         }
         if (any_leaves(!ok)) {   // and the list of odd tokens is complete
@@ -527,7 +546,7 @@ template <int KIND, int D>
 __device__ inline void mma_role(const PagedAttendArgs& a, Shared& sh, const Range& rg, uint32_t smem) {
     using C = TileCfg<D>;
     constexpr int kType = KIND == MKV_BF16 ? 1 : 0;
-    constexpr uint32_t qk = mma_desc(kType, kSub, false), pv = mma_desc(kType, D, true);
+    constexpr uint32_t qk = mma_desc(kType, kTile, false), pv = mma_desc(kType, D, true);
     auto bar = [](unsigned long long& b) { return ptx::smem_u32(&b); };
     uint32_t q_par = 0, q1_par = 0, p_par[2] = {0, 0};
     int tiles = 0;
@@ -536,25 +555,24 @@ __device__ inline void mma_role(const PagedAttendArgs& a, Shared& sh, const Rang
     const uint32_t tmem = sh.tmem;
     const uint32_t q_lo = (smem >> 4) | desc_lead(16), k_lo = ((smem + 2 * C::kHalf) >> 4) | desc_lead(16),
                    v_lo = ((smem + 4 * C::kHalf) >> 4) | desc_lead(128 * 128);
-    // S of half w, tokens 64 h .. of the stage, into its buffer h
-    auto qk_product = [&](int w, int stage, int h) {
+    auto qk_product = [&](int w, int stage) {
         if (one_lane()) {
-            const uint32_t a0 = q_lo + w * (C::kHalf >> 4), b0 = k_lo + stage * (C::kHalf >> 4) + h * (kSub * 128 >> 4), d = tmem + w * 128 + h * kSub;
+            const uint32_t a0 = q_lo + w * (C::kHalf >> 4), b0 = k_lo + stage * (C::kHalf >> 4), d = tmem + w * 128;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 constexpr uint32_t kChunk = 128 * 128 >> 4;
                 mma_ss(d, a0 + (k >> 2) * kChunk + (k & 3) * 2, b0 + (k >> 2) * kChunk + (k & 3) * 2, qk, k > 0);
             }
-            mma_commit(bar(sh.s_full[w][h]));
+            mma_commit(bar(sh.s_full[w]));
         }
         __syncwarp();
     };
+    // tokens 64 h .. of the tile
     auto pv_product = [&](int w, int stage, int h, bool add) {
         if (one_lane()) {
-            const uint32_t d = tmem + 256 + w * 128, a0 = tmem + w * 128 + h * kSub, b0 = v_lo + stage * (C::kHalf >> 4) + h * (kSub * 128 >> 4);
+            const uint32_t d = tmem + 256 + w * 128, a0 = tmem + w * 128 + h * 32, b0 = v_lo + stage * (C::kHalf >> 4) + h * (64 * 128 >> 4);
 #pragma unroll
-            for (int k = 0; k < kSub / 16; ++k) mma_ts(d, a0 + 8 * k, b0 + k * (2048 >> 4), pv, add || k > 0);
-            mma_commit(bar(sh.pv_done[w][h]));
+            for (int k = 0; k < 4; ++k) mma_ts(d, a0 + 8 * k, b0 + k * (2048 >> 4), pv, add || k > 0);
         }
         __syncwarp();
     };
@@ -576,30 +594,30 @@ __device__ inline void mma_role(const PagedAttendArgs& a, Shared& sh, const Rang
             }
             if (!ready(bar(sh.k_full[tiles & 1]), (tiles >> 1) & 1)) return;
             fence_after();
-            for (int w = 0; w < halves; ++w) qk_product(w, tiles & 1, 0);
+            for (int w = 0; w < halves; ++w) qk_product(w, tiles & 1);
+            commit(sh.k_empty[tiles & 1]);
         }
-        // Every S is issued one product ahead of the P that its row's threads are at: when they are done with one, the next
-        // is there.  (A buffer's new S is issued behind the product that read its old P: the unit runs them in order.)
 #pragma unroll 1
         for (int j = 0; j < nt; ++j) {
             const int t = tiles + j, stage = t & 1, next = (t + 1) & 1;
             const bool more = j + 1 < nt;
             if (!ready(bar(sh.v_full[stage]), (t >> 1) & 1)) return;
+            if (more && !ready(bar(sh.k_full[next]), ((t + 1) >> 1) & 1)) return;
 #pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                if (h == 1 && more && !ready(bar(sh.k_full[next]), ((t + 1) >> 1) & 1)) return;
-                fence_after();
-                for (int w = 0; w < halves; ++w) {
-                    if (h == 0) qk_product(w, stage, 1);
-                    else if (more) qk_product(w, next, 0);
-                    if (h == 0 && w == halves - 1) commit(sh.k_empty[stage]);
+            for (int w = 0; w < halves; ++w) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
                     if (!ready(bar(sh.p_full[w][h]), p_par[w])) return;
-                    if (h == 1) p_par[w] ^= 1;
                     fence_after();
                     pv_product(w, stage, h, j + h > 0);
                 }
+                p_par[w] ^= 1;
+                if (w == halves - 1) commit(sh.v_empty[stage]);
+                // the next S goes over this P, behind the product that reads it: the unit runs them in order
+                if (more) qk_product(w, next);
+                else commit(sh.o_full[w]);
             }
-            commit(sh.v_empty[stage]);
+            if (more) commit(sh.k_empty[next]);
         }
         tiles += nt;
         if (u.end() >= rg.t1 || !next_unit<kRows, kTile>(a, u)) return;
@@ -849,7 +867,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendArgs
     if (tid == 0) {
         auto init = [](unsigned long long& b, int n) { ptx::mbar_init(ptx::smem_u32(&b), n); };
         for (int i = 0; i < 2; ++i) {
-            init(sh.q_full[i], 128); init(sh.s_full[i][0], 1); init(sh.s_full[i][1], 1); init(sh.p_full[i][0], 128); init(sh.p_full[i][1], 128); init(sh.pv_done[i][0], 1); init(sh.pv_done[i][1], 1);
+            init(sh.q_full[i], 128); init(sh.s_full[i], 1); init(sh.p_full[i][0], 128); init(sh.p_full[i][1], 128); init(sh.o_full[i], 1);
             init(sh.k_full[i], KIND == MKV_INT4 ? 128 : 1); init(sh.v_full[i], KIND == MKV_INT4 ? 128 : 1);
             init(sh.k_empty[i], 1); init(sh.v_empty[i], 1);
         }
@@ -861,14 +879,26 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendArgs
     fence_before();
     __syncthreads();
     fence_after();
-    if (tid < kSoft) {
+    if (KIND == MKV_INT4) {
+        // 512 threads x 128 registers = 65536; 256 x 184 + 128 x 96 + 128 x 40 = 64512
+        if (tid < kSoft) {
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+            softmax_role<KIND, D, IO32>(a, sh, rg, smem);
+        } else if (tid < kSoft + 128) {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+            dequant_role<D>(a, sh, rg, smem, tid - kSoft);
+        } else {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+            if (warp == (kSoft + 128) / 32) mma_role<KIND, D>(a, sh, rg, smem);
+        }
+    } else if (tid < kSoft) {
+        // 384 threads x 168 registers = 64512 = 256 x 216 + 128 x 72
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         softmax_role<KIND, D, IO32>(a, sh, rg, smem);
-    } else if (KIND == MKV_INT4) {
-        if (tid < kSoft + 128) dequant_role<D>(a, sh, rg, smem, tid - kSoft);
-        else mma_role<KIND, D>(a, sh, rg, smem);
     } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (tid == kSoft) copy_role<D>(a, sh, rg, smem, &map, layer_rows);
-        else if (tid >= kSoft + 32) mma_role<KIND, D>(a, sh, rg, smem);
+        else if (warp == kSoft / 32 + 1) mma_role<KIND, D>(a, sh, rg, smem);
     }
     __syncwarp();
     fence_before();
