@@ -198,7 +198,7 @@ mkv_status mkv_paged_attend(mkv_paged* c, int layer, const void* q, int64_t q_st
     a.b = {starts, lens, table, n_tokens, batch, table_stride};
     a.q = q; a.q_stride = q_stride; a.out = out; a.lse = lse;
     a.max_new = starts ? max_new : 1;
-    a.window = window;
+    a.window = window < (1 << 30) ? window : 0;   // no sequence is longer than that
     a.scale_log2 = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)c->head_dim)));
     a.scratch = c->ws + paged_ws().scratch;
     const long long rows_per_layer = (long long)c->n_pages * 2 * c->kv_heads * c->page_size;

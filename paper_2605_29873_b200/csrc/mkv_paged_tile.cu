@@ -24,7 +24,6 @@
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cfloat>
-#include <climits>
 
 #include "mkv_paged_units.cuh"
 
@@ -38,8 +37,7 @@ constexpr unsigned kFull = 0xffffffffu;
 // diagonal and the window's edge), and the producers are at most three units ahead.
 constexpr int kOddMax = 2048;
 
-// 4 bits: two warpgroups of softmax, one that turns codes into rows, one for the MMA warp; registers are dealt out by need
-template <int KIND> __host__ __device__ constexpr int threads_of() { return kSoft + (KIND == MKV_INT4 ? 256 : 128); }
+template <int KIND> __host__ __device__ constexpr int threads_of() { return kSoft + (KIND == MKV_INT4 ? 128 + 32 : 64); }
 
 template <int D>
 struct TileCfg {
@@ -87,24 +85,33 @@ __device__ inline bool one_lane() {
 }
 #define MKV_R8(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
 #define MKV_I8(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
-// 32 columns of this thread's lane
-__device__ inline void tmem_ld32(uint32_t addr, uint32_t (&v)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
-        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : MKV_R8(v, 0), MKV_R8(v, 8), MKV_R8(v, 16), MKV_R8(v, 24) : "r"(addr));
-}
+// 16, 32, 64 columns of this thread's lane, there when the statement is done: between a load and a wait apart the
+// compiler may copy or spill the registers that are still to be written.
 __device__ inline void tmem_ld16(uint32_t addr, uint32_t (&v)[16]) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : MKV_R8(v, 0), MKV_R8(v, 8) : "r"(addr));
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : MKV_R8(v, 0), MKV_R8(v, 8) : "r"(addr) : "memory");
+}
+__device__ inline void tmem_ld32(uint32_t addr, uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : MKV_R8(v, 0), MKV_R8(v, 8), MKV_R8(v, 16), MKV_R8(v, 24) : "r"(addr) : "memory");
+}
+__device__ inline void tmem_ld64(uint32_t addr, uint32_t (&v)[32], uint32_t (&w)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%64];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%65];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : MKV_R8(v, 0), MKV_R8(v, 8), MKV_R8(v, 16), MKV_R8(v, 24), MKV_R8(w, 0), MKV_R8(w, 8), MKV_R8(w, 16), MKV_R8(w, 24)
+        : "r"(addr), "r"(addr + 32) : "memory");
 }
 __device__ inline void tmem_st16(uint32_t addr, const uint32_t (&v)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
         ::MKV_I8(v, 0), MKV_I8(v, 8), "r"(addr) : "memory");
 }
-__device__ inline void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ inline void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // fp32 accumulator, A and B both bf16 (1) or fp16 (0), M = 128, N columns; `b_outer`: B's outer dimension is contiguous
@@ -144,7 +151,9 @@ struct Shared {
     int dead;                       // a wait ran out: everybody leaves
     int n_odd;
     int2 odd[kOddMax];              // (tile of this CTA, position), a ring
-    float k_mul[2], v_exp[2];       // 4 bits: what the stage's K and V were divided by (a factor, a log2)
+    // 4 bits: what a tile's K and V were divided by (a factor, a log2), of the last four tiles: a K stage is free for the next
+    // tile as soon as its product is done, before the softmax has looked up its factor
+    float k_mul[4], v_exp[4];
     float red[8];
     FindShared find;
     Unit unit;                      // the first of this CTA
@@ -240,22 +249,35 @@ __device__ inline float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
     return y;
 }
-// The row's 128 logits, and the largest visible one of them (bottom < column <= top); others become -inf.
+// The row's logits go through registers 64 at a time, in loops that are not unrolled over the row: with a code path per
+// column the kernel's warps waited for instructions a fifth of the time.
+//
+// 64 logits from column `at` on; those not visible (bottom < column <= top) become -inf.
 template <bool EDGE>
-__device__ inline float row_logits(uint32_t sT, int top, int bottom, uint32_t (&x)[4][32]) {
+__device__ inline void hide64(int at, int top, int bottom, uint32_t (&x)[32], uint32_t (&y)[32]) {
+    if (!EDGE) return;
+    const int t = top - at, b = bottom - at;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) tmem_ld32(sT + 32 * c, x[c]);
-    wait_ld();
+    for (int e = 0; e < 32; ++e) {
+        if (e > t || e <= b) x[e] = 0xff800000u;
+        if (e + 32 > t || e + 32 <= b) y[e] = 0xff800000u;
+    }
+}
+// The largest visible logit; x and y hold the first 64 afterwards.
+template <bool EDGE>
+__device__ inline float row_max(uint32_t sT, int top, int bottom, uint32_t (&x)[32], uint32_t (&y)[32]) {
     float mx[4] = {kPagedNegInf, kPagedNegInf, kPagedNegInf, kPagedNegInf};
+#pragma unroll 1
+    for (int at = 64; at >= 0; at -= 64) {
+        tmem_ld64(sT + at, x, y);
+        hide64<EDGE>(at, top, bottom, x, y);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-#pragma unroll
-        for (int e = 0; e < 32; ++e)
-            if (EDGE && (32 * c + e > top || 32 * c + e <= bottom)) x[c][e] = 0xff800000u;
-#pragma unroll
-        for (int e = 0; e < 32; e += 8)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(x[c][e + 2 * k]), __uint_as_float(x[c][e + 2 * k + 1]));
+        for (int e = 0; e < 32; e += 4) {
+            mx[0] = max3(mx[0], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+            mx[1] = max3(mx[1], __uint_as_float(x[e + 2]), __uint_as_float(x[e + 3]));
+            mx[2] = max3(mx[2], __uint_as_float(y[e]), __uint_as_float(y[e + 1]));
+            mx[3] = max3(mx[3], __uint_as_float(y[e + 2]), __uint_as_float(y[e + 3]));
+        }
     }
     return fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
 }
@@ -303,17 +325,23 @@ __device__ inline void weights32(const uint32_t (&v)[32], uint32_t pT, uint64_t 
     }
     tmem_st16(pT, pk);
 }
-// Weights 2^(s * mul + ref) of 64 columns, 16 bits each, into tensor memory (over S, which has been read); returns their sum
-// once they are there.
+// The row's weights 2^(s * mul + ref), 16 bits each, over S in tensor memory; x and y hold the first 64 logits.  `ready` is told
+// of the first 64 and of the others.  Returns the sum of the weights.
 template <int KIND, bool EDGE>
-__device__ inline float row_weights(const uint32_t (&x)[32], const uint32_t (&y)[32], uint32_t pT, float mul, float ref) {
+__device__ inline float row_weights(uint32_t sT, float mul, float ref, int top, int bottom, uint32_t (&x)[32], uint32_t (&y)[32], uint32_t ready) {
     const uint64_t m2 = pair(mul, mul), r2 = pair(ref, ref);
     uint64_t sum[2] = {0, 0};
-    weights32<KIND, EDGE>(x, pT, m2, r2, sum);
-    weights32<KIND, EDGE>(y, pT + 16, m2, r2, sum);
+#pragma unroll 1
+    for (int h = 0; h < 2; ++h) {
+        weights32<KIND, EDGE>(x, sT + 32 * h, m2, r2, sum);
+        weights32<KIND, EDGE>(y, sT + 32 * h + 16, m2, r2, sum);
+        if (h == 0) tmem_ld64(sT + 64, x, y);
+        wait_st();
+        fence_before();
+        ptx::mbar_arrive(ready + 8 * h);
+        if (h == 0) hide64<EDGE>(64, top, bottom, x, y);
+    }
     const float2 s = unpair(add2(sum[0], sum[1]));
-    wait_st();
-    fence_before();
     return s.x + s.y;
 }
 
@@ -443,15 +471,15 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                 float mul = back, f = 0.f;
                 if (KIND == MKV_INT4) {
                     if (!(ok = __all_sync(kFull, wait_or_leave(a, sh, ptx::smem_u32(&sh.v_full[stage]), par)))) break;
-                    mul *= sh.k_mul[stage];
-                    f = sh.v_exp[stage];
+                    mul *= sh.k_mul[(tiles + j) & 3];
+                    f = sh.v_exp[(tiles + j) & 3];
                 }
                 if (!(ok = __all_sync(kFull, wait_or_leave(a, sh, s_full, s_par)))) break;
                 s_par ^= 1;
                 fence_after();
-                const int top = place.pos - t0, bottom = a.window > 0 ? top - a.window : INT_MIN;   // bottom < column <= top
-                uint32_t x[4][32];
-                float mx = edge ? row_logits<true>(sT, top, bottom, x) : row_logits<false>(sT, 0, 0, x);
+                const int top = place.pos - t0, bottom = a.window > 0 ? max(top - a.window, -1) : -1;   // bottom < column <= top
+                uint32_t x[32], y[32];
+                float mx = edge ? row_max<true>(sT, top, bottom, x, y) : row_max<false>(sT, 0, 0, x, y);
                 mx = fmaf(mx, mul, f);
                 const bool move = mx > m + 8.f;
                 if (__any_sync(kFull, move)) {
@@ -463,7 +491,6 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                         for (int c = 0; c < D / 16; ++c) {
                             uint32_t v[16];
                             tmem_ld16(oT + 16 * c, v);
-                            wait_ld();
 #pragma unroll
                             for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * sc);
                             tmem_st16(oT + 16 * c, v);
@@ -471,10 +498,8 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                     }
                 }
                 const float ref = f - m;
-                float sum = edge ? row_weights<KIND, true>(x[0], x[1], sT, mul, ref) : row_weights<KIND, false>(x[0], x[1], sT, mul, ref);
-                ptx::mbar_arrive(p_full);
-                sum += edge ? row_weights<KIND, true>(x[2], x[3], sT + 32, mul, ref) : row_weights<KIND, false>(x[2], x[3], sT + 32, mul, ref);
-                ptx::mbar_arrive(p_full + 8);
+                const float sum = edge ? row_weights<KIND, true>(sT, mul, ref, top, bottom, x, y, p_full)
+                                       : row_weights<KIND, false>(sT, mul, ref, 0, 0, x, y, p_full);
                 l += KIND == MKV_INT4 ? sum * ex2(-f) : sum;
             }
         }
@@ -500,7 +525,6 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                 if (nt > 0) {
                     uint32_t v[32];
                     tmem_ld32(oT + 32 * c, v);
-                    wait_ld();
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(v[e]);
                 } else {
@@ -675,37 +699,42 @@ struct RawTile {
     uint32_t ks[NG], kl[NG / 2], vs[NG], vl[NG];
 };
 
-template <int D, bool K, bool V>
-__device__ inline void load_raw(const PagedAttendArgs& a, const Unit& u, int t0, int id, RawTile<D>& x) {
-    constexpr int NG = D / 32;
-    // K: token t0 + id.  V: pair of tokens t0 + 2 (id / 2), its lower or upper half of the words
+// Where a thread's words of a tile are: K of token t0 + id; of V, for the pair of tokens t0 + id & ~1, the lower or upper half.
+// k == nullptr: nobody sees that block.
+struct RawRows { const uint4 *k, *v; const uint32_t* par; int r; };
+template <int D>
+__device__ inline RawRows raw_rows(const PagedAttendArgs& a, const Unit& u, int t0, int id) {
     const int p = t0 + id;
-#pragma unroll
-    for (int i = 0; i < NG; ++i) {
-        if (K) { x.k[i] = make_uint4(0, 0, 0, 0); x.ks[i] = 0; x.kl[i / 2] = 0; }
-        if (V) { x.v[i] = make_uint4(0, 0, 0, 0); x.vs[i] = x.vl[i] = 0; }
-    }
-    if ((p & ~15) > u.phi) return;
+    if ((p & ~15) > u.phi) return {nullptr, nullptr, nullptr, 0};
     const uint8_t* head = a.c.pages + (size_t)paged_page(a.c, a.b, u.s, p & ~15) * a.c.page_bytes + (size_t)u.h * a.c.head_bytes;
     const int row = p & ((1 << a.c.page_shift) - 1), r = row & 15;
     const uint8_t* blk = head + (size_t)(row >> 4) * paged_block_bytes(D);
-    const uint4* kp = reinterpret_cast<const uint4*>(blk + r * (D / 2));
-    const uint4* vp = reinterpret_cast<const uint4*>(blk + 8 * D + (r >> 1) * D + (r & 1) * (D / 2));
+    return {reinterpret_cast<const uint4*>(blk + r * (D / 2)), reinterpret_cast<const uint4*>(blk + 8 * D + (r >> 1) * D + (r & 1) * (D / 2)),
+            reinterpret_cast<const uint32_t*>(blk + 16 * D), r};
+}
+template <int D>
+__device__ inline void load_k_params(const RawRows& w, RawTile<D>& x) {
+    constexpr int NG = D / 32;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        if (K) x.k[i] = __ldg(kp + i);
-        if (V) x.v[i] = __ldg(vp + i);
-    }
-    const uint32_t* par = reinterpret_cast<const uint32_t*>(blk + 16 * D);
+    for (int j = 0; j < NG; ++j) x.ks[j] = w.k ? __ldg(w.par + (w.r >> 1) * NG + j) : 0u;
+#pragma unroll
+    for (int j = 0; j < NG / 2; ++j) x.kl[j] = w.k ? __ldg(w.par + 8 * NG + w.r * (NG / 2) + j) : 0u;
+}
+template <int D>
+__device__ inline void load_v_params(const RawRows& w, RawTile<D>& x) {
+    constexpr int NG = D / 32;
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
-        if (K) x.ks[j] = __ldg(par + (r >> 1) * NG + j);
-        if (V) x.vs[j] = __ldg(par + 16 * NG + (r >> 1) * NG + j);
-        if (V) x.vl[j] = __ldg(par + 24 * NG + (r >> 1) * NG + j);
+        x.vs[j] = w.k ? __ldg(w.par + 16 * NG + (w.r >> 1) * NG + j) : 0u;
+        x.vl[j] = w.k ? __ldg(w.par + 24 * NG + (w.r >> 1) * NG + j) : 0u;
     }
+}
+// A tile's words move up as they are used, and the next tile's come in behind them, a whole tile ahead of their use.
+template <int D>
+__device__ inline void shift_in(uint4 (&x)[D / 32], const uint4* next, int i) {
 #pragma unroll
-    for (int j = 0; j < NG / 2; ++j)
-        if (K) x.kl[j] = __ldg(par + 8 * NG + r * (NG / 2) + j);
+    for (int k = 0; k + 1 < D / 32; ++k) x[k] = x[k + 1];
+    x[D / 32 - 1] = next ? __ldg(next + i) : make_uint4(0, 0, 0, 0);
 }
 
 __device__ inline __half2 codes_low(uint32_t w) {    // nibbles 0 and 4 as numbers
@@ -755,7 +784,14 @@ __device__ inline void dequant_role(const PagedAttendArgs& a, Shared& sh, const 
             const int stage = tiles & 1;
             const uint32_t par = ((tiles >> 1) & 1) ^ 1;
             const int t0 = (first + j) * kTile;
-            if (fresh) { load_raw<D, true, true>(a, u, t0, id, x); fresh = false; }
+            if (fresh) {
+                const RawRows w = raw_rows<D>(a, u, t0, id);
+                load_k_params<D>(w, x);
+                load_v_params<D>(w, x);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) { shift_in<D>(x.k, w.k, i); shift_in<D>(x.v, w.v, i); }
+                fresh = false;
+            }
             const int begin = a.window > 0 ? max(0, u.plo - a.window + 1) : 0;
             const int p = t0 + id;
             const bool seen = p <= u.phi && p >= begin, other = (p ^ 1) <= u.phi && (p ^ 1) >= begin;
@@ -772,24 +808,28 @@ __device__ inline void dequant_role(const PagedAttendArgs& a, Shared& sh, const 
             const float kf = tile_exponent(sh, id, ktop);
             const float kdown = __uint_as_float((uint32_t)(127 - (int)kf) << 23);
             if (tiles >= 2) wait_or_leave(a, sh, ptx::smem_u32(&sh.k_empty[stage]), par);   // goes on even then: its threads stay together
-            if (id == 0) sh.k_mul[stage] = __uint_as_float((uint32_t)(127 + (int)kf) << 23);
+            if (id == 0) sh.k_mul[tiles & 3] = __uint_as_float((uint32_t)(127 + (int)kf) << 23);
             const uint32_t ktile = smem + (2 + stage) * C::kHalf;
+            const RawRows next = j + 1 < nt ? raw_rows<D>(a, u, t0 + kTile, id) : RawRows{nullptr, nullptr, nullptr, 0};
+            __half2 s2[NG], l2[NG];
 #pragma unroll
+            for (int g = 0; g < NG; ++g) { s2[g] = __float2half2_rn(s[g] * kdown); l2[g] = __float2half2_rn(l[g] * kdown); }
+            load_k_params<D>(next, x);
+#pragma unroll 1
             for (int i = 0; i < D / 32; ++i) {
                 // 16 bytes = words (t, j): for D = 128 t = i, j = 0..3; for D = 64 t = 2 i + e / 2, j = e & 1
-                const uint32_t w4[4] = {x.k[i].x, x.k[i].y, x.k[i].z, x.k[i].w};
+                const uint32_t w4[4] = {x.k[0].x, x.k[0].y, x.k[0].z, x.k[0].w};
+                shift_in<D>(x.k, next.k, i);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int t = NG == 4 ? i : 2 * i + (e >> 1), g = e & (NG - 1);
-                    const __half2 s2 = __float2half2_rn(s[g] * kdown), l2 = __float2half2_rn(l[g] * kdown);
                     const uint32_t w = w4[e];
-                    sts128(chunk_at(ktile, id, 4 * g + t), as_u32(__hfma2(codes_low(w), s2, l2)), as_u32(__hfma2(codes_high(w), s2, l2)),
-                           as_u32(__hfma2(codes_low(w >> 8), s2, l2)), as_u32(__hfma2(codes_high(w >> 8), s2, l2)));
+                    sts128(chunk_at(ktile, id, 4 * g + t), as_u32(__hfma2(codes_low(w), s2[g], l2[g])), as_u32(__hfma2(codes_high(w), s2[g], l2[g])),
+                           as_u32(__hfma2(codes_low(w >> 8), s2[g], l2[g])), as_u32(__hfma2(codes_high(w >> 8), s2[g], l2[g])));
                 }
             }
             ptx::fence_proxy_async();
             ptx::mbar_arrive(ptx::smem_u32(&sh.k_full[stage]));
-            if (j + 1 < nt) load_raw<D, true, false>(a, u, t0 + kTile, id, x);
             // ---- V: tokens id & ~1 and its neighbour, words of g 0..3 or 4..7
             const bool even_seen = id & 1 ? other : seen, odd_seen = id & 1 ? seen : other;
             float vtop = 0.f, s0[NG], l0[NG], s1[NG], l1[NG];
@@ -810,32 +850,38 @@ __device__ inline void dequant_role(const PagedAttendArgs& a, Shared& sh, const 
             const float vf = tile_exponent(sh, id, vtop);
             const float vdown = __uint_as_float((uint32_t)(127 - (int)vf) << 23);
             if (tiles >= 2) wait_or_leave(a, sh, ptx::smem_u32(&sh.v_empty[stage]), par);
-            if (id == 0) sh.v_exp[stage] = vf;
+            if (id == 0) sh.v_exp[tiles & 3] = vf;
             if ((id & 1) == 0 && (odd0 || odd1)) {
                 if (odd0) sh.odd[atomicAdd(&sh.n_odd, 1) % kOddMax] = make_int2(tiles, p);
                 if (odd1) sh.odd[atomicAdd(&sh.n_odd, 1) % kOddMax] = make_int2(tiles, p + 1);
             }
             const uint32_t vtile = smem + (4 + stage) * C::kHalf;
+            __half2 vs2[NG], vl2[NG];   // halves: even token, odd token
 #pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                vs2[g] = __floats2half2_rn(s0[g] * vdown, s1[g] * vdown);
+                vl2[g] = __floats2half2_rn(l0[g] * vdown, l1[g] * vdown);
+            }
+            load_v_params<D>(next, x);
+#pragma unroll 1
             for (int i = 0; i < D / 32; ++i) {
                 // words (g, j): for D = 128 g = g0 + i, j = 0..3; for D = 64 g = g0 + 2 i + e / 2, j = e & 1
-                const uint32_t w4[4] = {x.v[i].x, x.v[i].y, x.v[i].z, x.v[i].w};
+                const uint32_t w4[4] = {x.v[0].x, x.v[0].y, x.v[0].z, x.v[0].w};
+                shift_in<D>(x.v, next.v, i);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int g = g0 + (NG == 4 ? i : 2 * i + (e >> 1)), j = e & (NG - 1);
-                    const __half2 s2 = __floats2half2_rn(s0[j] * vdown, s1[j] * vdown), l2 = __floats2half2_rn(l0[j] * vdown, l1[j] * vdown);
+                    const int g = g0 + (NG == 4 ? i : 2 * i + (e >> 1)), jj = e & (NG - 1);
                     const uint32_t w = w4[e];
-                    // halves: even token, odd token; four channels
-                    const uint32_t c0 = as_u32(__hfma2(codes_low(w), s2, l2)), c1 = as_u32(__hfma2(codes_high(w), s2, l2));
-                    const uint32_t c2 = as_u32(__hfma2(codes_low(w >> 8), s2, l2)), c3 = as_u32(__hfma2(codes_high(w >> 8), s2, l2));
+                    // four channels
+                    const uint32_t c0 = as_u32(__hfma2(codes_low(w), vs2[jj], vl2[jj])), c1 = as_u32(__hfma2(codes_high(w), vs2[jj], vl2[jj]));
+                    const uint32_t c2 = as_u32(__hfma2(codes_low(w >> 8), vs2[jj], vl2[jj])), c3 = as_u32(__hfma2(codes_high(w >> 8), vs2[jj], vl2[jj]));
                     const uint32_t off = (g & 1) * 8;
-                    sts64(chunk_at(vtile, r0, 4 * j + (g >> 1)) + off, __byte_perm(c0, c1, 0x5410), __byte_perm(c2, c3, 0x5410));
-                    sts64(chunk_at(vtile, r0 + 1, 4 * j + (g >> 1)) + off, __byte_perm(c0, c1, 0x7632), __byte_perm(c2, c3, 0x7632));
+                    sts64(chunk_at(vtile, r0, 4 * jj + (g >> 1)) + off, __byte_perm(c0, c1, 0x5410), __byte_perm(c2, c3, 0x5410));
+                    sts64(chunk_at(vtile, r0 + 1, 4 * jj + (g >> 1)) + off, __byte_perm(c0, c1, 0x7632), __byte_perm(c2, c3, 0x7632));
                 }
             }
             ptx::fence_proxy_async();
             ptx::mbar_arrive(ptx::smem_u32(&sh.v_full[stage]));
-            if (j + 1 < nt) load_raw<D, false, true>(a, u, t0 + kTile, id, x);
         }
         if (u.end() >= rg.t1 || !next_unit<kRows, kTile>(a, u)) return;
         part_of(u, first, nt);
@@ -880,23 +926,12 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap map, const PagedAttendArgs
     __syncthreads();
     fence_after();
     if (KIND == MKV_INT4) {
-        // 512 threads x 128 registers = 65536; 256 x 184 + 128 x 96 + 128 x 40 = 64512
-        if (tid < kSoft) {
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
-            softmax_role<KIND, D, IO32>(a, sh, rg, smem);
-        } else if (tid < kSoft + 128) {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-            dequant_role<D>(a, sh, rg, smem, tid - kSoft);
-        } else {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-            if (warp == (kSoft + 128) / 32) mma_role<KIND, D>(a, sh, rg, smem);
-        }
+        if (tid < kSoft) softmax_role<KIND, D, IO32>(a, sh, rg, smem);
+        else if (tid < kSoft + 128) dequant_role<D>(a, sh, rg, smem, tid - kSoft);
+        else mma_role<KIND, D>(a, sh, rg, smem);
     } else if (tid < kSoft) {
-        // 384 threads x 168 registers = 64512 = 256 x 216 + 128 x 72
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         softmax_role<KIND, D, IO32>(a, sh, rg, smem);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (tid == kSoft) copy_role<D>(a, sh, rg, smem, &map, layer_rows);
         else if (warp == kSoft / 32 + 1) mma_role<KIND, D>(a, sh, rg, smem);
     }
