@@ -42,9 +42,8 @@ template <int KIND> __host__ __device__ constexpr int threads_of() { return kSof
 template <int D>
 struct TileCfg {
     static constexpr int kHalf = 128 * D * 2;         // 128 rows of 16-bit channels: Q half, K tile, V tile
-    // rows on their way out, 8 KB a warp: over Q, or behind everything where Q's rows are shorter than that
-    static constexpr int kOut = D == 128 ? 0 : 6 * kHalf;
-    static constexpr int kSmem = 1024 + 6 * kHalf + (D == 128 ? 0 : 65536);    // Q0 Q1, K x 2, V x 2
+    static constexpr int kOut = 6 * kHalf;               // rows on their way out, 2 KB a warp
+    static constexpr int kSmem = 1024 + 6 * kHalf + 16384;   // Q0 Q1, K x 2, V x 2
 };
 
 // ---- tcgen05 and friends
@@ -193,43 +192,45 @@ __device__ inline RowPlace row_place(const PagedAttendArgs& a, const Unit& u, in
     return {u.len - u.n + j, u.tok0 + j, head, (size_t)(u.tok0 + j) * a.c.q_heads + head};
 }
 
-// The rows of a warp on their way out: every lane has its row's 16-byte chunks put() into the warp's 8 KB of shared
-// memory (that of its Q rows, free by then; chunk c of row r at c ^ (r & 15)), then 16 lanes write 256 bytes of
-// a row at a time.
+// The rows of a warp on their way out, 64 bytes of each at a time: every lane has its row's four 16-byte chunks put() into the
+// warp's 2 KB of shared memory (chunk c of row r at c ^ (r / 2 & 3): no bank twice), then four lanes write a row's.
 struct RowsOut {
     uint32_t slice;
     int lane;
     __device__ void put(int c, uint32_t x, uint32_t y, uint32_t z, uint32_t w) const {
-        sts128(slice + lane * 256 + ((c ^ (lane & 15)) << 4), x, y, z, w);
+        sts128(slice + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4), x, y, z, w);
     }
-    // bytes: of a row that were put (<= 256).  `dst`: this lane's row, or nullptr
-    __device__ void flush(uint8_t* dst, int bytes) const {
+    // `dst`: where this lane's 64 bytes go, or nullptr
+    __device__ void flush(uint8_t* dst) const {
         __syncwarp();
-#pragma unroll 4
-        for (int i = 0; i < 32; i += 2) {
-            const int r = i + (lane >> 4), c = lane & 15;
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+            const int r = i + (lane >> 2), c = lane & 3;
             uint8_t* p = reinterpret_cast<uint8_t*>(__shfl_sync(kFull, reinterpret_cast<unsigned long long>(dst), r));
-            if (p && 16 * c < bytes) *reinterpret_cast<uint4*>(p + 16 * c) = lds128(slice + r * 256 + ((c ^ (r & 15)) << 4));
+            if (p) *reinterpret_cast<uint4*>(p + 16 * c) = lds128(slice + r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
         }
         __syncwarp();
     }
 };
 
-// 32 channels of every lane's row, o / l; a row is complete after the last.  `dst`: this lane's row, or nullptr
+// 32 channels of every lane's row, o / l.  `dst`: this lane's row, or nullptr
 template <int D>
 __device__ inline void store32(const PagedAttendArgs& a, const RowsOut& out, uint8_t* dst, int c, const float (&o)[32], float inv) {
     if (a.c.out_f32) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            out.put((c & 32) / 4 + i, __float_as_uint(o[4 * i] * inv), __float_as_uint(o[4 * i + 1] * inv), __float_as_uint(o[4 * i + 2] * inv),
-                    __float_as_uint(o[4 * i + 3] * inv));
-        if (c & 32) out.flush(dst ? dst + (c - 32) * 4 : nullptr, 256);
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 4 * h; i < 4 * h + 4; ++i)
+                out.put(i & 3, __float_as_uint(o[4 * i] * inv), __float_as_uint(o[4 * i + 1] * inv), __float_as_uint(o[4 * i + 2] * inv),
+                        __float_as_uint(o[4 * i + 3] * inv));
+            out.flush(dst ? dst + c * 4 + 64 * h : nullptr);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            out.put(c / 8 + i, ptx::pack_bf16x2(o[8 * i] * inv, o[8 * i + 1] * inv), ptx::pack_bf16x2(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
+            out.put(i, ptx::pack_bf16x2(o[8 * i] * inv, o[8 * i + 1] * inv), ptx::pack_bf16x2(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
                     ptx::pack_bf16x2(o[8 * i + 4] * inv, o[8 * i + 5] * inv), ptx::pack_bf16x2(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
-        if (c == D - 32) out.flush(dst, D * 2);
+        out.flush(dst ? dst + c * 2 : nullptr);
     }
 }
 
@@ -355,11 +356,27 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
     const uint32_t sT = sh.tmem + lanes + w * 128, oT = sh.tmem + lanes + 256 + w * 128;
     const uint32_t q_full = ptx::smem_u32(&sh.q_full[w]), p_full = ptx::smem_u32(&sh.p_full[w][0]);   // two: the first 64 columns, the others
     const uint32_t s_full = ptx::smem_u32(&sh.s_full[w]), o_full = ptx::smem_u32(&sh.o_full[w]);
-    const RowsOut rows_out{smem + C::kOut + (tid >> 5) * 8192, lane};
+    const RowsOut rows_out{smem + C::kOut + (tid >> 5) * 2048, lane};
     const uint32_t q_smem = smem + w * C::kHalf, v_smem = smem + 4 * C::kHalf;
     uint32_t s_par = 0, o_par = 0;
     int tiles = 0;            // of this CTA so far: stage and parity of K and V
     Unit u = sh.unit;
+    // bf16 Q: the warp's 32 rows of a unit, copied straight into place, D / 8 lanes for a row.  Asked for as soon as the unit
+    // before has no more use for Q, so that it arrives beside that one's last product and its result's way out.
+    auto ask_q = [&](const Unit& y) {
+        constexpr int kPer = D / 8, kAt = 32 / kPer;
+        const RowPlace pl = row_place(a, y, w * 128 + row);
+        const int c = lane % kPer;
+#pragma unroll 4
+        for (int i = 0; i < 32; i += kAt) {
+            const int rr = i + lane / kPer;
+            const int tok = __shfl_sync(kFull, pl.tok, rr), head = __shfl_sync(kFull, pl.head, rr);
+            const __nv_bfloat16* src = (const __nv_bfloat16*)a.q + (size_t)tok * a.q_stride + (size_t)head * D + 8 * c;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(chunk_at(q_smem, warp4 * 32 + rr, c)), "l"(src),
+                         "r"(warp_row + rr < y.rows ? 16 : 0) : "memory");
+        }
+    };
+    if (KIND == MKV_BF16 && u.nblk > 0 && (w == 0 || u.rows > 128)) ask_q(u);
     for (;;) {
         const long long lo = max(u.base, rg.t0), hi = min(u.end(), rg.t1);
         const int first = u.blk0 + (int)(lo - u.base), nt = u.nblk == 0 ? 0 : (int)(hi - lo);
@@ -369,7 +386,10 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
         const bool live = r < u.rows;
         float m = -FLT_MAX, l = 0.f, back = a.scale_log2;
         if (nt > 0 && active) {
-            // ---- Q: the warp's 32 rows, D / 8 lanes for a row, all loads on their way before the first is used
+            if (KIND == MKV_BF16) {
+                asm volatile("cp.async.wait_all;" ::: "memory");
+            } else {
+            // ---- Q over 4-bit pages: the warp's 32 rows, D / 8 lanes for a row, all loads on their way before the first is used
             constexpr int kPer = D / 8, kAt = 32 / kPer, kN = 32 / kAt;   // lanes of a row, rows at a time, times
             const int c = lane % kPer;
             constexpr int kWords = KIND == MKV_INT4 && IO32 ? 2 : 1;
@@ -391,9 +411,7 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int rr = (i0 + i) * kAt + lane / kPer, row16 = warp4 * 32 + rr;
-                if (KIND == MKV_BF16) {
-                    sts128(chunk_at(q_smem, row16, c), x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w);
-                } else {
+                {
                     // fp16, scaled by a power of two to [2^13, 2^14); channels of eight in the order 0 4 1 5 2 6 3 7, as
                     // the codes' nibbles come (K has the same order)
                     float y[8];
@@ -419,6 +437,7 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                     const float mine = __shfl_sync(kFull, up, (lane % kAt) * kPer);
                     if (lane / kAt == i0 + i) back = a.scale_log2 * (1.f / mine);
                 }
+            }
             }
             }
             ptx::fence_proxy_async();
@@ -503,6 +522,12 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
                 l += KIND == MKV_INT4 ? sum * ex2(-f) : sum;
             }
         }
+        const bool last = u.end() >= rg.t1;
+        Unit next = u;
+        if (!last) {
+            next_unit<kRows, kTile>(a, next);
+            if (KIND == MKV_BF16 && ok && next.nblk > 0 && (w == 0 || next.rows > 128)) ask_q(next);   // S of the last tile is there: Q is free
+        }
         if (active && nt > 0 && ok) {
             ok = wait_or_leave(a, sh, o_full, o_par);
             o_par ^= 1;
@@ -557,11 +582,11 @@ __device__ inline void softmax_role(const PagedAttendArgs& a, Shared& sh, const 
             if (live && !whole) { *part.m(r) = m; *part.l(r) = l; }
         }
         tiles += nt;
-        if (u.end() >= rg.t1) {
+        if (last) {
             if (tid == 0) leave_join(a, rg, u);
             return;
         }
-        next_unit<kRows, kTile>(a, u);
+        u = next;
     }
 }
 
