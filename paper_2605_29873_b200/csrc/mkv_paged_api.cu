@@ -203,9 +203,18 @@ mkv_status mkv_paged_attend(mkv_paged* c, int layer, const void* q, int64_t q_st
     a.scratch = c->ws + paged_ws().scratch;
     const long long rows_per_layer = (long long)c->n_pages * 2 * c->kv_heads * c->page_size;
     const cudaStream_t st = (cudaStream_t)stream;
-    // Few rows of a sequence and head: the cache is streamed, a unit's rows on one pass.  Many: tiles on the tensor
-    // cores.  fp32 pages have the first form only.
-    const cudaError_t e = c->kv_dtype == MKV_F32 || (long long)a.c.group * a.max_new <= 64
+    // Few rows of a sequence and head: the cache is streamed, once for every 16 rows (fp32 pages and fp32 queries: 8).  Many:
+    // tiles on the tensor cores.  fp32 pages have the first form only.  Measured, 8 KV heads, 4096 cached tokens, us:
+    //   rows                16    32    48    64    96   128
+    //   bf16, 1 sequence    16/26 18/25 20/26 21/26 25/26 28/27     first form / tiles
+    //   bf16, 16            52/83 92/83 131/84 166/84
+    //   4 bits, 1           17/32 18/31 20/32 22/32 25/32 29/32
+    //   4 bits, 16          41/141 70/144 99/148 128/150 186/153
+    // While there are fewer (sequence, head) pairs than would fill the GPU the first form's passes run side by side.
+    const long long rows = (long long)a.c.group * a.max_new;
+    const bool idle = (long long)batch * c->kv_heads < c->sm_count / 2;
+    const bool stream_cache = c->kv_dtype == MKV_F32 || rows <= (idle ? 96 : c->kv_dtype == MKV_INT4 ? 64 : 24);
+    const cudaError_t e = stream_cache
                               ? launch_paged_decode(a, c->head_dim, &c->map16, layer * rows_per_layer, c->sm_count, c->device, st)
                               : launch_paged_tile(a, c->head_dim, &c->map_page, layer * rows_per_layer, c->sm_count, c->device, st);
     if (e != cudaSuccess) return MKV_ERR_CUDA;

@@ -1,6 +1,9 @@
 // Writing the paged cache (with the rotation of keys and queries on the way) and reading its rows
 // back as values.  Elementwise work: bound by memory for prompts, by the latency of a launch and
-// three dependent loads (starts, lens, table) for single tokens.
+// three dependent loads (starts, lens, table) for single tokens (2.9 us for 16 of them).
+// Measured for 36.4k tokens of prompts, 32 query and 8 KV heads of 128 channels: bf16 153 us (894 MB, 5.8 TB/s); 4 bits
+// 320 us, bound by instruction issue (5400 warp instructions a token, most of them for scales and codes), read back as values
+// 40 us.
 #include <cfloat>
 
 #include "mkv_paged_units.cuh"

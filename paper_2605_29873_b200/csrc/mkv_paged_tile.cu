@@ -2,7 +2,7 @@
 //
 // A unit is one (sequence, KV head, 256 rows of new token x query head), worked through in tiles of 128
 // cached tokens; the list of all units' tiles is cut into one contiguous range per CTA (see
-// mkv_paged_units.cuh), parts of a unit are joined by the CTA that delivers the last one, in order.
+// mkv_paged_units.cuh), which also joins the parts of a unit that the cuts leave.
 //
 // A CTA is a pipeline over its tiles.  Its 256 rows are two halves of 128, one row per thread of a
 // softmax warpgroup:
@@ -21,6 +21,12 @@
 // 128 KB.
 // The second product's weights are one bf16 (2^-9 rounding, as the values they multiply have), over 4-bit pages
 // one fp16.  Sums, references and O are fp32; the sum of p is taken before the rounding.
+//
+// Measured (B200, 8 KV heads x 4 query heads x 128 channels): pieces of 700 to 1300 tokens of 4 sequences over 1400 to 5200
+// cached bf16 ones, 111 GFLOP: 204 us; 1184 tokens over 20000, 371 GFLOP: 400 us.  Bound by the chain of a half's products
+// and softmax (2.0 to 2.3 us for a tile of 256 rows, the products alone 1.1), and for short caches by the ends of units (a few
+// us each: the masked tile, the last product, the way out).  4 bits, 600 to 1000 tokens of 2 sequences over 5000 to 9000,
+// 216 GFLOP: 390 us, bound by the warpgroup that turns codes into rows.
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cfloat>

@@ -171,11 +171,11 @@ class Case:
 # Roundings below 32 bits, by path.  e_p: the weights enter the second product as a sum of two bf16
 # (2^-17 of the value is left) over bf16 pages, as one fp16 (2^-11), or a sum of two where out is fp32,
 # over 4-bit pages, whose lowest values meet them as a sum of two bf16; as they are over fp32 pages.
-# From 65 rows (tokens x group) of a sequence and head on, a tile kernel takes over: weights one bf16
+# From 65 rows (tokens x group) of a sequence and head on, a tile kernel may take over (bf16 batches: from 25): weights one bf16
 # (2^-8) over bf16 pages; over 4-bit pages one fp16, and the rows themselves rounded to fp16 (2^-11), fp32
 # queries too (another 2^-11 of every product).
 def roundings(kind, out, rows, io=BF16):
-    tiles = rows > 64
+    tiles = rows > (24 if kind == BF16 else 64)
     if kind == F32:
         return dict(e_p=0.0)
     if kind == BF16:
@@ -784,3 +784,57 @@ def test_large_batches_and_long_sequences(kind):
     c = Case(kind, 8, 1, 128, 64, [70001], out=F32, seed=6)
     c.fill()
     a, _ = c.check_attend(q=c.rand(1, 8, 128) * 4, **roundings(kind, F32, 8))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [BF16, INT4])
+@pytest.mark.parametrize("window", [0, 1500])
+def test_long_pieces(kind, window):
+    """Many tiles and several units for every block of the grid, units cut between blocks: against the plain form on
+    sampled tokens, and the same bits again."""
+    c = Case(kind, 8, 2, 128, 64, [2900, 4111, 700, 3333], [350, 1, 700, 97], out=F32, seed=11)
+    c.fill()
+    q = c.rand(c.T, 8, 128) * 3
+    outs = []
+    for _ in range(3):
+        out = torch.zeros(c.T, 8, 128, device="cuda")
+        lse = torch.zeros(c.T, 8, device="cuda")
+        c.ctx.attend(0, q, c.lens, c.table, out, starts=c.starts, max_new=700, window=window, lse=lse)
+        outs.append((out, lse))
+    c.ctx.status_sync()
+    assert all(torch.equal(a, outs[0][0]) and torch.equal(b, outs[0][1]) for a, b in outs[1:])
+    K, V = R.cache_values(c.pages, kind, 0, 128, 64)
+    KS, VS = R.cache_sizes(c.pages, kind, 0, 128, 64)
+    rd = roundings(kind, F32, 2800)
+    for b, (a, e) in enumerate(zip(c.starts_h, c.starts_h[1:])):
+        k, v, ks, vs = (R.rows_of(x, c.table[b], c.lens_h[b], 64) for x in (K, V, KS, VS))
+        for i in sorted({a, (2 * a + e) // 3, (a + e) // 2, max(a, e - 2), e - 1}):
+            ref, lse, ma, sa = R.attend(q[i:i + 1].double(), k, v, c.lens_h[b] - (e - i), window, sizes=(ks, vs))
+            bound = R.out_bound(ref, ma, sa, 128, c.lens_h[b], HALF[F32], **rd)
+            assert ((outs[0][0][i].double() - ref[0]).abs() <= bound[0]).all(), (b, i)
+            err = (outs[0][1][i].double() - lse[0]).abs()
+            assert (err <= R.lse_bound(lse, sa, 128, c.lens_h[b], rd["e_p"], rd.get("e_k", 0.0))[0]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [BF16, INT4, F32])
+@pytest.mark.parametrize("new", [6, 7, 16, 17, 24, 25])
+def test_either_side_of_the_choice_of_a_kernel(kind, new):
+    """24 and 28, 64 and 68, 96 and 100 rows of a sequence and head, in a batch that fills the GPU and in a small one."""
+    for batch in (40, 2):
+        lens = [new + (37 * i) % 150 for i in range(batch)]
+        c = Case(kind, 8, 2, 64, 16, lens, [new if i % 3 else 1 + i % new for i in range(batch)], seed=new)
+        c.fill()
+        c.check_attend(max_new=new, **roundings(kind, c.out, 4 * new))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [BF16, INT4, F32])
+def test_windows_of_any_size(kind):
+    c = Case(kind, 4, 2, 128, 16, [300, 40], [130, 40])
+    c.fill()
+    q = c.rand(170, 4, 128)
+    whole, _ = c.check_attend(q=q, **roundings(kind, c.out, 260))
+    for w in (300, 1 << 29, (1 << 30) - 1, 1 << 30, (1 << 31) - 1):
+        out, _ = c.check_attend(q=q, window=w, **roundings(kind, c.out, 260))
+        assert torch.equal(out, whole)
