@@ -120,49 +120,64 @@ __device__ __noinline__ Coded quantise8_wide(const double (&x)[8]) {
 __device__ inline float min_nan(float a, float b) { float y; asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
 __device__ inline float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
 
-// The same in 32 bits, where that decides it: x[i] is within err[i] of the exact value (short16: is a bf16).  *unsure: some
+// The same in 32 bits, where that decides it: x is within err of the exact values (short16: they are bf16).  *unsure: some
 // rounding (of the scale, the lowest value, a code) could go either way; the warp then takes the 64-bit
 // form (about one rotated group in a thousand).
-__device__ inline Coded quantise8(const float (&x)[8], const float (&err)[8], bool short16, bool* unsure) {
-    float lo = x[0], hi = x[0], e = err[0];
+__device__ inline Coded quantise8(const float (&x)[8], float err, bool short16, bool* unsure) {
+    float lo = x[0], hi = x[0];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) { lo = min_nan(lo, x[i]); hi = max_nan(hi, x[i]); e = fmaxf(e, err[i]); }
+    for (int i = 1; i < 8; ++i) { lo = min_nan(lo, x[i]); hi = max_nan(hi, x[i]); }
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) {
         lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
         hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-        e = fmaxf(e, __shfl_xor_sync(0xffffffffu, e, o));
+        err = fmaxf(err, __shfl_xor_sync(0xffffffffu, err, o));
     }
     Coded r;
-    const float t = hi * (1.f / 15.f) - lo * (1.f / 15.f);
-    const float te = e * (2.f / 15.f) + (fabsf(hi) + fabsf(lo)) * 1.5e-8f + t * 1.2e-7f;   // 1/15 and its products are 2^-23 off at most
+    const float t = hi * (1.f / 15.f) - lo * (1.f / 15.f), size = fabsf(hi) + fabsf(lo);
+    const float te = err * (2.f / 15.f) + size * 1.5e-8f + t * 1.2e-7f;   // 1/15 and its products are 2^-23 off at most
     const __nv_bfloat16 sb = __float2bfloat16_rn(t), lb = __float2bfloat16_rn(lo);
     bool u = __bfloat16_as_ushort(__float2bfloat16_rn(t - te)) != __bfloat16_as_ushort(__float2bfloat16_rn(t + te)) ||
-             __bfloat16_as_ushort(__float2bfloat16_rn(lo - e)) != __bfloat16_as_ushort(__float2bfloat16_rn(lo + e)) ||
+             __bfloat16_as_ushort(__float2bfloat16_rn(lo - err)) != __bfloat16_as_ushort(__float2bfloat16_rn(lo + err)) ||
              t < 1e-35f;   // and scales whose reciprocal or differences leave the normal range
     r.scale = __bfloat16_as_ushort(sb);
     r.lowest = __bfloat16_as_ushort(lb);
     const float s = __bfloat162float(sb), l = __bfloat162float(lb), inv = __frcp_rn(s);
-    r.codes = 0;
+    // n = rint((x - l) / s), 1.5 * 2^23 more puts it into the lowest bits; right unless x - l - n s is next to s / 2.  The
+    // codes are gathered with the bits of the constant, which come off at the end.
+    constexpr float kOne = 12582912.f;
+    const float half = 0.5f * s, close = err + size * 2.4e-7f;
+    bool near = false;
+    uint32_t all = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        // k = floor((x - l) / s), or one less or more where that is next to a whole number; then on which side of
-        // (k + 1/2) s, an exact product, x - l lies.  1.5 * 2^23 puts k into the lowest bits.
-        constexpr float kOne = 12582912.f;
+    for (int i = 7; i >= 0; --i) {
         const float d = x[i] - l;
-        const float k = fminf(fmaxf(fmaf(d, inv, -0.5f) + kOne, kOne), kOne + 14.f);
-        const float rest = fmaf(-((k - kOne) + 0.5f), s, d);
-        uint32_t code = __float_as_uint(k) & 15u;
-        if (rest > 0.f) code += 1;
-        if (fabsf(rest) <= fabsf(d) * 1.2e-7f) {
-            // on the border, as far as the difference is exact: that of two bf16 is, unless their sizes are far apart.  A
-            // tie goes to the even code.
-            if (rest == 0.f) code += code & 1u;
-            const float big = fmaxf(fabsf(x[i]), fabsf(l)), small = fminf(fabsf(x[i]), fabsf(l));
-            u |= !short16 || (small != 0.f && small * 16384.f < big);
+        const float k = fminf(fmaxf(fmaf(d, inv, kOne), kOne), kOne + 15.f);
+        near |= fabsf(fabsf(fmaf(-(k - kOne), s, d)) - half) <= close;
+        all = all * 16u + __float_as_uint(k);
+    }
+    r.codes = all - 0x4b400000u * 0x11111111u;
+    if (near) {
+        r.codes = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            // k = floor((x - l) / s), or one less or more where that is next to a whole number; then on which side of
+            // (k + 1/2) s, an exact product, x - l lies
+            const float d = x[i] - l;
+            const float k = fminf(fmaxf(fmaf(d, inv, -0.5f) + kOne, kOne), kOne + 14.f);
+            const float rest = fmaf(-((k - kOne) + 0.5f), s, d);
+            uint32_t code = __float_as_uint(k) & 15u;
+            if (rest > 0.f) code += 1;
+            if (fabsf(rest) <= fabsf(d) * 1.2e-7f) {
+                // on the border, as far as the difference is exact: that of two bf16 is, unless their sizes are far apart.  A
+                // tie goes to the even code.
+                if (rest == 0.f) code += code & 1u;
+                const float big = fmaxf(fabsf(x[i]), fabsf(l)), small = fminf(fabsf(x[i]), fabsf(l));
+                u |= !short16 || (small != 0.f && small * 16384.f < big);
+            }
+            u |= fabsf(rest) < err;
+            r.codes |= code << (4 * i);
         }
-        u |= fabsf(rest) < err[i];
-        r.codes |= code << (4 * i);
     }
     *unsure = u;
     if (!(fabsf(lo) <= FLT_MAX && fabsf(hi) <= FLT_MAX)) { r.codes = 0; r.scale = 0x7fc0; r.lowest = 0; *unsure = false; }
@@ -294,6 +309,7 @@ __global__ void __launch_bounds__(kAppendThreads, KIND == MKV_INT4 ? 3 : 5) page
         const bool up = c >= half;
         const int other = up ? c - half : c + half;
         const int pair0 = a.interleaved ? c >> 1 : up ? c - half : c;
+        const float sign = up ? 1.f : -1.f;
         for (int h0 = (tid >> 5) * kHeads; h0 < hk2; h0 += kAppendThreads / 32 * kHeads) {
             const int h = h0 + lane / kLanes;
             const bool in = h < hk2, is_v = in && h >= a.c.kv_heads;
@@ -323,20 +339,29 @@ __global__ void __launch_bounds__(kAppendThreads, KIND == MKV_INT4 ? 3 : 5) page
                     if (k == 1 && role != 2) break;
                     const float (&x)[8] = xs[k];
                     const float (&o)[8] = os[k];
-                    float y[8], err[8];
+                    float y[8], err = 0.f;
                     if (turn) {
+                        const float2* const w = cs[t0 + k] + (pair0 >> 3) * 2 + (a.interleaved ? (l & 1) * 2 * (D / 8) : 0);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float2 f = cs[t0 + k][cs_at<D>(pair0 + (a.interleaved ? e >> 1 : e))];
-                            const float p = a.interleaved ? x[e ^ 1] : o[e];
-                            const bool second = a.interleaved ? (e & 1) : up;
-                            const float ps = p * f.y;
-                            y[e] = fmaf(x[e], f.x, second ? ps : -ps);
-                            err[e] = (fabsf(x[e]) + fabsf(p)) * 4.8e-7f;   // cos and sin 2^-22 off, the product and the sum rounded: 2^-21
+                        for (int e = 0; e < 8; e += 2) {
+                            // two pairs of angles as one piece; neighbours: one pair of channels each, so half the pieces
+                            if (a.interleaved) {
+                                const float2 f = w[(e >> 2) * (D / 8) + ((e >> 1) & 1)];
+                                const float x0 = x[e], x1 = x[e + 1];
+                                y[e] = fmaf(x0, f.x, -(x1 * f.y));
+                                y[e + 1] = fmaf(x1, f.x, x0 * f.y);
+                                err = fmaxf(err, fabsf(x0) + fabsf(x1));
+                            } else {
+                                const float4 f = *reinterpret_cast<const float4*>(w + (e >> 1) * (D / 8));
+                                y[e] = fmaf(x[e], f.x, o[e] * (sign * f.y));
+                                y[e + 1] = fmaf(x[e + 1], f.z, o[e + 1] * (sign * f.w));
+                                err = fmaxf(err, fmaxf(fabsf(x[e]) + fabsf(o[e]), fabsf(x[e + 1]) + fabsf(o[e + 1])));
+                            }
                         }
+                        err *= 4.8e-7f;   // cos and sin 2^-22 off, the product and the sum rounded: 2^-21
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) { y[e] = x[e]; err[e] = 0.f; }
+                        for (int e = 0; e < 8; ++e) y[e] = x[e];
                     }
                     bool unsure;
                     z[k] = quantise8(y, err, sizeof(T) == 2 && !turn, &unsure);
