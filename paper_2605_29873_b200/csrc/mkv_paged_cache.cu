@@ -2,8 +2,7 @@
 // back as values.  Elementwise work: bound by memory for prompts, by the latency of a launch and
 // three dependent loads (starts, lens, table) for single tokens (2.9 us for 16 of them).
 // Measured for 36.4k tokens of prompts, 32 query and 8 KV heads of 128 channels: bf16 153 us (894 MB, 5.8 TB/s); 4 bits
-// 320 us, bound by instruction issue (5400 warp instructions a token, most of them for scales and codes), read back as values
-// 40 us.
+// 239 us, bound by instruction issue, most of it for scales and codes; read back as values 40 us.
 #include <cfloat>
 
 #include "mkv_paged_units.cuh"
@@ -465,10 +464,18 @@ __global__ void __launch_bounds__(kAppendThreads) paged_read_kernel(const PagedR
 
 template <typename T, int KIND, int D>
 cudaError_t append_t(const PagedAppendArgs& a, cudaStream_t st) {
-    constexpr int TT = 4;
+    // Tokens of a block: one while there are few (latency: 2.9 us for 16), then as many as keep the GPU full.  4 bits, us:
+    // 2048 tokens 20 by eights, 27 by sixteens; 36.4k tokens (with the read-back) 336 by fours, 295 by eights, 279 by sixteens.
+    // bf16: 36.4k tokens 153 by fours, 155 by eights.
     const unsigned y = KIND == MKV_INT4 && a.q ? 2 : 1;
-    if (a.b.n_tokens <= 1024) return paged_launch(paged_append_kernel<T, KIND, D, 1>, dim3(a.b.n_tokens, y), kAppendThreads, 0, st, a);
-    return paged_launch(paged_append_kernel<T, KIND, D, TT>, dim3((a.b.n_tokens + TT - 1) / TT, y), kAppendThreads, 0, st, a);
+    auto go = [&](auto kernel, int tt) { return paged_launch(kernel, dim3((a.b.n_tokens + tt - 1) / tt, y), kAppendThreads, 0, st, a); };
+    if (a.b.n_tokens <= 1024) return go(paged_append_kernel<T, KIND, D, 1>, 1);
+    if constexpr (KIND != MKV_INT4) {
+        return go(paged_append_kernel<T, KIND, D, 4>, 4);
+    } else {
+        if (a.b.n_tokens <= 16384) return go(paged_append_kernel<T, KIND, D, 8>, 8);
+        return go(paged_append_kernel<T, KIND, D, 16>, 16);
+    }
 }
 template <typename T, int KIND, int D>
 cudaError_t read_t(const PagedReadArgs& a, cudaStream_t st) {

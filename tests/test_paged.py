@@ -199,6 +199,7 @@ APPEND = [
     (INT4, F32, 128, 4, 4, 256, [500, 3], [500, 3], 48, False, None),
     (INT4, BF16, 128, 8, 1, 64, [2000], [1999], 0, False, None),   # more than 1024 tokens, odd offset
     (BF16, None, 128, 2, 1, 64, [1500], [1333], 128, False, None),
+    (INT4, BF16, 64, 2, 2, 32, [9001, 8000], [9000, 7997], 64, True, None),   # more than 16384 tokens
 ]
 
 
