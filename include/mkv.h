@@ -479,11 +479,11 @@ mkv_status mkv_paged_set_rotation(mkv_paged* ctx, const float* inv_freq, int rot
 /* Stores the new tokens' keys (rotated) and values in the cache, and writes the rotated queries.
  *   q     [n_tokens] rows of [q_heads][head_dim] io_dtype, q_stride elements apart; NULL: none
  *   k, v  [n_tokens] rows of [kv_heads][head_dim], likewise (the three may be slices of one buffer)
- *   q_out [n_tokens][q_heads][head_dim], may be q itself where q_stride is q_heads * head_dim;
- *         NULL exactly when q is
+ *   q_out [n_tokens][q_heads][head_dim], may be q itself where q_stride is q_heads * head_dim and must
+ *         not overlap the inputs otherwise; NULL exactly when q is
  *   positions  device int32 [n_tokens], what the rotation takes for the tokens' positions; NULL:
  *         their positions in the cache
- * Pointers 16-byte aligned, strides multiples of 16 bytes.  Tokens of a sequence that has fewer
+ * Pointers 16-byte aligned (the int32 arrays 4-byte), strides multiples of 16 bytes.  Tokens of a sequence that has fewer
  * tokens in the cache than new ones (lens < starts[b + 1] - starts[b]) have no place for the first
  * of them; those are passed over, their q_out rows too.
  * Errors: INVALID_ARG, CAPACITY (batch > max_batch), CUDA. */
@@ -495,7 +495,7 @@ mkv_status mkv_paged_append(mkv_paged* ctx, int layer, const void* q, int64_t q_
 /* Attention of the new tokens' queries over the cache (which holds the new tokens already): the
  * token at position t sees the positions j <= t, with window > 0 those with j > t - window.
  *   q    rows as in mkv_paged_append, rotated already
- *   out  [n_tokens][q_heads][head_dim], out_dtype
+ *   out  [n_tokens][q_heads][head_dim], out_dtype; must not overlap q
  *   lse  float [n_tokens][q_heads] or NULL: log of the sum of exp(scale * q . k) over the seen tokens
  *   max_new  the most new tokens any sequence has (a promise: a sequence with more sets
  *        MKV_ERR_CAPACITY and its results are undefined); ignored where starts is NULL

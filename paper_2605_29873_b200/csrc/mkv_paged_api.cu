@@ -76,6 +76,7 @@ PagedDev dev_of(const mkv_paged* c, int layer) {
 mkv_status batch_args(const mkv_paged* c, int layer, int n_tokens, int batch, const int32_t* starts,
                       const int32_t* lens, const int32_t* table, int table_stride) {
     if (!c || layer < 0 || layer >= c->layers || n_tokens < 0 || batch < 0) return MKV_ERR_INVALID_ARG;
+    if (((uintptr_t)starts | (uintptr_t)lens | (uintptr_t)table) & 3u) return MKV_ERR_INVALID_ARG;   // int32 arrays
     if (batch > c->max_batch) return MKV_ERR_CAPACITY;
     if (!starts && n_tokens != batch) return MKV_ERR_INVALID_ARG;
     if (n_tokens > 0 && batch == 0) return MKV_ERR_INVALID_ARG;
@@ -166,7 +167,7 @@ mkv_status mkv_paged_append(mkv_paged* c, int layer, const void* q, int64_t q_st
     if (s != MKV_OK) return s;
     if (n_tokens == 0) return MKV_OK;
     if (!strided_ok(c, k, k_stride, c->kv_heads) || !strided_ok(c, v, v_stride, c->kv_heads)) return MKV_ERR_INVALID_ARG;
-    if ((q != nullptr) != (q_out != nullptr)) return MKV_ERR_INVALID_ARG;
+    if ((q != nullptr) != (q_out != nullptr) || ((uintptr_t)positions & 3u)) return MKV_ERR_INVALID_ARG;
     if (q && (!strided_ok(c, q, q_stride, c->q_heads) || !aligned16(q_out))) return MKV_ERR_INVALID_ARG;
     DeviceGuard guard(c->device);
     if (!guard.ok) return MKV_ERR_CUDA;
@@ -228,7 +229,7 @@ mkv_status mkv_paged_read(mkv_paged* c, int layer, int batch, const int32_t* fir
     if (s != MKV_OK) return s;
     if (rows < 0) return MKV_ERR_INVALID_ARG;
     if (rows == 0 || batch == 0) return MKV_OK;
-    if (!K || !V || !aligned16(K) || !aligned16(V)) return MKV_ERR_INVALID_ARG;
+    if (!K || !V || !aligned16(K) || !aligned16(V) || ((uintptr_t)first & 3u)) return MKV_ERR_INVALID_ARG;
     DeviceGuard guard(c->device);
     if (!guard.ok) return MKV_ERR_CUDA;
     PagedReadArgs a;

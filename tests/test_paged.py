@@ -611,7 +611,7 @@ def test_refusals_of_the_calls():
 
     for kw in [dict(layer=1), dict(layer=-1), dict(n=-1), dict(b=-1), dict(n=3), dict(k=None), dict(v=None), dict(qo=None),
                dict(q=None), dict(qs=511), dict(ks=255), dict(vs=260), dict(k=p + 2), dict(qo=p + 8), dict(ln=None),
-               dict(tb=None), dict(ts=0)]:
+               dict(tb=None), dict(ts=0), dict(ln=ln + 2), dict(tb=tb + 1), dict(st=p + 2)]:
         assert app(**kw) == 1, kw
     assert app(n=3, b=3) == 3 and app(ts=1 << 27) == 5
     assert app(n=0, b=0) == 0
@@ -632,7 +632,7 @@ def test_refusals_of_the_calls():
         a.update(kw)
         return L.mkv_paged_read(h, a["layer"], a["b"], a["first"], a["ln"], a["tb"], a["ts"], a["K"], a["V"], a["rows"], None)
 
-    for kw in [dict(layer=2), dict(rows=-1), dict(K=None), dict(V=p + 4), dict(ln=None)]:
+    for kw in [dict(layer=2), dict(rows=-1), dict(K=None), dict(V=p + 4), dict(ln=None), dict(first=p + 2)]:
         assert rd(**kw) == 1, kw
     assert rd(rows=0) == 0 and rd(b=3) == 3
     f = (C.c_float * 64)()
